@@ -113,6 +113,8 @@ typedef struct defl_opts {
                             X <- a_0 X + a_1 (X X^T) X + ... + a_d (X X^T)^d X with d = poly_terms - 1 (4 = the
                             degree-seven member); the schedule is then [L][poly_terms]. The polynomial in the Gram
                             matrix is formed by Horner steps, one more short-side product per degree beyond the quintic. */
+  const float* grad_scale; /* Muon step: device, NULL or a factor of Grad (defl_grad_norm's out + 1): Mom <- mu Mom + c Grad, the
+                            product c Grad rounded to fp32. c = 0 takes Grad as zeros, whatever it holds. */
 } defl_opts;
 
 typedef struct defl_info {
@@ -303,6 +305,74 @@ int defl_fill_gaussian(defl_ctx* ctx, void* dst, size_t count, int dtype, uint64
  * split the batch), DEFL_ERR_CUDA. */
 #define DEFL_NOALLOC_MAX_BATCH 256
 int defl_frobenius_norms_noalloc(const void* X, int dtype, int b, long long count, float* norms, void* cuda_stream);
+
+/* ---- What the rest of a training step needs: the parameters that Muon does not take -------------------------------
+ *
+ * AdamW over a list of tensors (embeddings, gains, biases, heads), in one launch per combination of types:
+ *   g <- c * g                                   c = *grad_scale (1 if NULL); c = 0 leaves the whole step out
+ *   m <- beta1 m + (1 - beta1) g                 v <- beta2 v + (1 - beta2) g^2
+ *   p <- (1 - lr * weight_decay) p - lr * (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ * in fp32 whatever the types; t is the number of this step, counted from 1. The hyperparameters are doubles because 1 - 0.999f
+ * is 1.3e-5 of itself away from 0.001. All pointers are device memory; the tensors of a list do not overlap one another
+ * (the same one twice is a race; the Python binding refuses it). A tensor with n = 0 or g = NULL is left alone.
+ *
+ * Moments in 8 bits (state_bits = 8): blocks of 256 consecutive elements of a tensor (the last one may be shorter), m and
+ * sqrt(v) held as e4m3 numbers times a fp32 scale per block, its largest magnitude / 448. The root and not v itself: its
+ * range in a block, 2.3e5, is that of m, so that the quotient of a small element is made of numbers that are both still
+ * there; and a root that is not zero never becomes zero, since m / eps would follow. Blocks whose largest magnitude is below
+ * 2^-100 count as zero; a gradient that is not finite makes its block's state NaN (defl_grad_norm's factor prevents it).
+ * The update itself uses the moments before they are rounded.
+ *
+ * Rounding. stochastic = 0: to nearest. An e4m3 number's neighbours are 6 to 12 % away and v moves by at most (1 - beta2) g^2
+ * in a step, so that rounding to nearest keeps an element where it stands within its block until a gradient some ten times its
+ * root comes along. stochastic != 0: y = |x| * 448 / largest goes to d * floor(y / d + u), d the spacing at y and u = 16
+ * random bits / 65536: right on average, at the price of noise (17 % of the root, v 5 % high, with Gaussian gradients of one size
+ * and beta2 = 0.999). bf16 weights are
+ * then rounded the same way, by the bits of the root (without it a step below 2^-9 of a weight is lost). The bits of
+ * elements 2j and 2j + 1 of list entry i are the halves of h(h(h(h(seed) ^ t) ^ i) ^ j), h as at defl_fill_gaussian: the low
+ * 16 bits of an element's half for m, the high 16 for the root and a bf16 weight. */
+typedef struct defl_adamw_tensor {
+  void* p;               /* weights, p_dtype, updated in place */
+  const void* g;         /* gradient, g_dtype, not modified; NULL: the tensor is left alone */
+  void* m;               /* first moment: fp32, or e4m3 with state_bits = 8; updated in place */
+  void* v;               /* second moment: fp32, or its root as e4m3; updated in place */
+  float* m_scale;        /* state_bits = 8: [ceil(n / 256)] fp32 scales, updated in place; else unused */
+  float* v_scale;
+  void* copy;            /* NULL, or [n] bf16: receives the new weights rounded to nearest (the forward pass's copy) */
+  int64_t n;             /* number of elements */
+  int p_dtype, g_dtype;  /* DEFL_F32 or DEFL_BF16 */
+  int state_bits;        /* 32 or 8 */
+} defl_adamw_tensor;
+
+typedef struct defl_adamw_opts {
+  double lr, beta1, beta2, eps, weight_decay;
+  int64_t step;               /* t >= 1, unless step_dev is given */
+  const int64_t* step_dev;    /* device, NULL or t (defl_grad_norm can count it): a captured graph then advances by itself */
+  const float* lr_dev;        /* device, NULL or the learning rate, in place of lr */
+  const float* grad_scale;    /* device, NULL or the factor c (defl_grad_norm's out + 1) */
+  uint64_t seed;              /* of the stochastic rounding */
+  int stochastic;
+} defl_adamw_opts;
+
+/* Errors: DEFL_ERR_ARG (null pointers, bad types, a step below 1, hyperparameters out of range), DEFL_ERR_RANK (more than
+ * 4e12 elements), DEFL_ERR_CUDA. Tensors that do not all start on 16-byte boundaries take single accesses: right, and slower. */
+int defl_adamw_step(defl_ctx* ctx, const defl_adamw_tensor* tensors, int count, const defl_adamw_opts* opts);
+
+/* Global norm of a list of gradients and what follows from it, without the host:
+ *   out[0] = sqrt(sum of all squares)            out[1] = min(1, max_norm / (out[0] + 1e-6)), 1 if max_norm <= 0
+ * A norm that is Inf or NaN makes out[1] zero (defl_adamw_step then leaves its step out) and *step stays; else *step, if
+ * given, is advanced by one: the number of the step that follows. Sums are in fp64, in an order that only the sizes decide.
+ *   tensors  host, `count` of them (n = 0 is skipped);  out  device, [2] fp32;  step  device, NULL or one int64
+ *   work     device, defl_grad_norm_work_bytes(count) bytes, 8-byte aligned, of this call alone until it is through: calls that
+ *            may run at the same time (two streams, two captured graphs) need one each
+ * Errors: DEFL_ERR_ARG, DEFL_ERR_RANK (more than 1.7e13 elements), DEFL_ERR_CUDA. */
+typedef struct defl_norm_tensor {
+  const void* x;
+  int64_t n;
+  int dtype;             /* DEFL_F32 or DEFL_BF16 */
+} defl_norm_tensor;
+size_t defl_grad_norm_work_bytes(int count);
+int defl_grad_norm(defl_ctx* ctx, const defl_norm_tensor* tensors, int count, float max_norm, float* out, int64_t* step, void* work);
 
 /* Diagnostics: one batched product C[b,M,N] = alpha * opA(A) opB(B) through a chosen engine, used by the
  * tests to check the tensor-core tile engine against the fp32 engine (no counterpart in the paper).

@@ -6,8 +6,10 @@ CUDA kernels. There is no fallback: if the shared library is missing the import 
 `lib()` fails, and without a CUDA device every compute call raises.
 """
 import ctypes
+import operator
 import os
 
+import numpy as np
 import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -27,7 +29,7 @@ EXPORTS = [
     "defl_create", "defl_destroy", "defl_set_stream", "defl_polar_workspace_bytes", "defl_psd_workspace_bytes",
     "defl_polar_window", "defl_psd_window", "defl_polar_batched", "defl_polar_batched_host", "defl_muon_step_batched", "defl_brsvd_batched", "defl_psd_project", "defl_inv_root", "defl_admm_diag_sdp", "defl_fill_gaussian", "defl_debug_gemm",
     "defl_frobenius_norms_noalloc", "defl_set_profiling", "defl_get_stage_ms", "defl_get_stage_ms_sum", "defl_launch_count", "defl_device_wait_status",
-    "defl_status_string", "defl_last_error",
+    "defl_status_string", "defl_last_error", "defl_adamw_step", "defl_grad_norm", "defl_grad_norm_work_bytes",
 ]
 
 
@@ -36,7 +38,19 @@ class DeflOpts(ctypes.Structure):
                 ("gamma", ctypes.c_float), ("norm_mode", ctypes.c_int), ("lanczos_start", ctypes.c_void_p),
                 ("warmup", ctypes.c_int), ("engine", ctypes.c_int), ("exploit_symmetry", ctypes.c_int),
                 ("tau", ctypes.c_float), ("half_filter", ctypes.c_int), ("bf16_iterates", ctypes.c_int),
-                ("poly_terms", ctypes.c_int)]
+                ("poly_terms", ctypes.c_int), ("grad_scale", ctypes.c_void_p)]
+
+
+class DeflAdamwOpts(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("step", ctypes.c_int64), ("step_dev", ctypes.c_void_p), ("lr_dev", ctypes.c_void_p),
+                ("grad_scale", ctypes.c_void_p), ("seed", ctypes.c_uint64), ("stochastic", ctypes.c_int)]
+
+
+# the tables of defl_adamw_tensor and defl_norm_tensor entries, laid out as the C compiler does
+_ADAMW_TENSOR = np.dtype([(n, np.uint64) for n in ("p", "g", "m", "v", "m_scale", "v_scale", "copy")] +
+                         [("n", np.int64), ("p_dtype", np.int32), ("g_dtype", np.int32), ("state_bits", np.int32)], align=True)
+_NORM_TENSOR = np.dtype([("x", np.uint64), ("n", np.int64), ("dtype", np.int32)], align=True)
 
 
 class DeflInfo(ctypes.Structure):
@@ -87,6 +101,10 @@ def lib():
                                       ctypes.c_void_p, ctypes.c_longlong, ctypes.c_longlong, ctypes.c_longlong,
                                       ctypes.c_void_p, ctypes.c_longlong, ctypes.c_longlong, ctypes.c_longlong,
                                       ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_float, ctypes.c_int]
+        L.defl_adamw_step.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.POINTER(DeflAdamwOpts)]
+        L.defl_grad_norm_work_bytes.restype = ctypes.c_size_t
+        L.defl_grad_norm_work_bytes.argtypes = [ctypes.c_int]
+        L.defl_grad_norm.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_float] + [ctypes.c_void_p] * 3
         L.defl_set_profiling.argtypes = [ctypes.c_void_p, ctypes.c_int]
         L.defl_get_stage_ms.argtypes = [ctypes.c_void_p, ctypes.POINTER(ctypes.c_float), ctypes.c_int]
         L.defl_get_stage_ms_sum.argtypes = [ctypes.c_void_p, ctypes.POINTER(ctypes.c_float), ctypes.c_int, ctypes.c_int]
@@ -158,6 +176,80 @@ def defl_psd_window(n, w, w_prime):
     return k.value, K.value
 
 
+def _gradients(grads, sizes, device):
+    """(addresses, type codes) of a list of gradients after its checks; None entries (no gradient this step) are 0 and float32.
+    Whole-list passes: a loop over the checks takes three times as long, and lists of hundreds of small tensors are bound by it."""
+    if any(g is None for g in grads):
+        some = [i for i, g in enumerate(grads) if g is not None]
+        ptr, dt = _gradients([grads[i] for i in some], None if sizes is None else [sizes[i] for i in some], device)
+        ptrs, codes = [0] * len(grads), [F32] * len(grads)
+        for i, p, d in zip(some, ptr, dt):
+            ptrs[i], codes[i] = p, d
+        return ptrs, codes
+    T = torch.Tensor
+    if set(map(T.get_device, grads)) - {device.index} or not all(map(T.is_contiguous, grads)):
+        raise ValueError("gradients must be contiguous tensors on %s" % device)
+    if sizes is not None and list(map(T.numel, grads)) != sizes:
+        raise ValueError("a gradient has another number of elements than its parameter")
+    codes = [_GRADIENT_CODE.get(d, -1) for d in map(_dtype_of, grads)]
+    if -1 in codes:
+        raise TypeError("gradients must be float32 or bfloat16")
+    return list(map(T.data_ptr, grads)), codes
+
+
+_dtype_of = operator.attrgetter("dtype")
+_GRADIENT_CODE = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+class AdamWGroup:
+    """The tensors of defl_adamw_step, checked once: parameters (float32 or bfloat16), first and second moments of the same
+    sizes, all float32 or, in 8 bits, float8_e4m3fn with float32 scales [ceil(n / 256)] (the second moment is held as its
+    root); optional bfloat16 copies of the parameters. The group keeps the tensors alive; no two of them may overlap."""
+
+    def __init__(self, params, exp_avg, exp_avg_sq, avg_scale=None, root_scale=None, copies=None):
+        self.params, self.exp_avg, self.exp_avg_sq = list(params), list(exp_avg), list(exp_avg_sq)
+        count = len(self.params)
+        none = [None] * count
+        self.avg_scale = list(avg_scale) if avg_scale is not None else none
+        self.root_scale = list(root_scale) if root_scale is not None else none
+        self.copies = list(copies) if copies is not None else none
+        lists = (self.params, self.exp_avg, self.exp_avg_sq, self.avg_scale, self.root_scale, self.copies)
+        if any(len(x) != count for x in lists):
+            raise ValueError("the lists of an AdamWGroup must have one entry per parameter")
+        self.device = self.params[0].device if count else None
+        self.sizes = [p.numel() for p in self.params]
+        self.table = np.zeros(count, dtype=_ADAMW_TENSOR)
+        spans = []
+        for i, (p, m, v, ms, vs, c) in enumerate(zip(*lists)):
+            n, eight = p.numel(), m.dtype == torch.float8_e4m3fn
+            if p.dtype not in (torch.float32, torch.bfloat16):
+                raise TypeError("parameter %d must be float32 or bfloat16" % i)
+            if m.dtype != v.dtype or m.dtype not in (torch.float32, torch.float8_e4m3fn):
+                raise TypeError("moments %d must both be float32 or both float8_e4m3fn" % i)
+            if eight and (ms is None or vs is None):
+                raise ValueError("moments %d in 8 bits need their scales" % i)
+            want = [(p, n, None, "parameter"), (m, n, None, "first moment"), (v, n, None, "second moment")]
+            if eight:
+                blocks = (n + 255) // 256
+                want += [(ms, blocks, torch.float32, "first moment's scales"), (vs, blocks, torch.float32, "second moment's scales")]
+            if c is not None:
+                want.append((c, n, torch.bfloat16, "copy"))
+            for t, size, dtype, what in want:
+                if not t.is_cuda or t.device != self.device or not t.is_contiguous():
+                    raise ValueError("%s %d must be a contiguous tensor on %s" % (what, i, self.device))
+                if t.numel() != size or (dtype is not None and t.dtype != dtype):
+                    raise ValueError("%s %d must have %d elements%s" % (what, i, size, " of " + str(dtype) if dtype else ""))
+                if size:
+                    spans.append((t.data_ptr(), t.data_ptr() + size * t.element_size(), "%s %d" % (what, i)))
+            ptr = lambda t: t.data_ptr() if t is not None else 0  # noqa: E731
+            self.table[i] = (ptr(p), 0, ptr(m), ptr(v), ptr(ms) if eight else 0, ptr(vs) if eight else 0, ptr(c), n, _dtype_code(p), F32,
+                             8 if eight else 32)
+        spans.sort()
+        for a, b in zip(spans, spans[1:]):
+            if b[0] < a[1]:
+                raise ValueError("%s and %s overlap" % (a[2], b[2]))
+
+
 class Context:
     """defl_ctx bound to one CUDA device; work is enqueued on torch's current stream at call time."""
 
@@ -190,8 +282,9 @@ class Context:
 
     def _opts(self, sketch=None, seed=0, restore_mode=RESTORE_PADDED, gamma=0.0, norm_mode=NORM_LANCZOS,
               lanczos_start=None, warmup=False, engine=ENGINE_AUTO, exploit_symmetry=False, tau=0.0, half_filter=False, bf16_iterates=False,
-              poly_terms=0):
+              poly_terms=0, grad_scale=None):
         o = DeflOpts()
+        o.grad_scale = self._scalar(grad_scale, torch.float32, 2, "grad_scale").data_ptr() + 4 if grad_scale is not None else None
         o.sketch = sketch.data_ptr() if sketch is not None else None
         o.seed = seed
         o.restore_mode = restore_mode
@@ -245,9 +338,10 @@ class Context:
     def defl_muon_step_batched(self, W, Mom, Grad, lr, mu, k, oversample, power_iters, coeff_schedule, steps=None,
                                nesterov=False, weight_decay=0.0, scale=1.0, sketch=None, seed=0,
                                restore_mode=RESTORE_PADDED, gamma=0.0, engine=ENGINE_AUTO, exploit_symmetry=False,
-                               tau=0.0):
+                               tau=0.0, grad_scale=None):
         """One Deflated Muon step on a shape group, in place: Mom <- mu Mom + Grad (Grad may be None),
-        W <- (1 - lr wd) W - lr scale F(Mom or its Nesterov look-ahead), F = defl_polar_batched's map."""
+        W <- (1 - lr wd) W - lr scale F(Mom or its Nesterov look-ahead), F = defl_polar_batched's map. grad_scale:
+        defl_grad_norm's result, whose factor multiplies Grad."""
         _dev(W, "W"), _dev(Mom, "Mom")
         if Mom.ndim != 3 or W.shape != Mom.shape:
             raise ValueError("W and Mom must be [b, m, n] of the same shape")
@@ -262,7 +356,7 @@ class Context:
             if sketch.dtype != torch.float32:
                 raise TypeError("sketch must be float32")
         opts = self._opts(sketch=sketch, seed=seed, restore_mode=restore_mode, gamma=gamma, engine=engine,
-                          exploit_symmetry=exploit_symmetry, tau=tau)
+                          exploit_symmetry=exploit_symmetry, tau=tau, grad_scale=grad_scale)
         self._sync_stream()
         rc = lib().defl_muon_step_batched(self._h, _ptr(W), _dtype_code(W), _ptr(Mom), _ptr(Grad) if Grad is not None else None,
                                           b, m, n, _dtype_code(Mom), lr, mu, int(bool(nesterov)), weight_decay, scale,
@@ -392,6 +486,56 @@ class Context:
                                       k, _ptr(warm_basis), K, sched, T, ctypes.byref(opts), res)
         self._check(rc)
         return y, torch.tensor(list(res)[:3 * iters], dtype=torch.float32).reshape(iters, 3)
+
+    def defl_adamw_step(self, group, grads, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, grad_scale=None,
+                        stochastic=False, seed=0):
+        """One AdamW step, in place, over an AdamWGroup; grads: one tensor per parameter (None: left alone this step), float32 or
+        bfloat16. step: this step's number from 1, or an int64 CUDA tensor [1] that holds it; lr: a number or a float32 CUDA
+        tensor [1]; grad_scale: defl_grad_norm's result, whose factor multiplies the gradients (0: the step is left out)."""
+        if group.device is not None and group.device != self.device:
+            raise ValueError("the group's tensors are on %s, the context is on %s" % (group.device, self.device))
+        if len(grads) != len(group.sizes):
+            raise ValueError("%d gradients for %d parameters" % (len(grads), len(group.sizes)))
+        table = group.table
+        table["g"], table["g_dtype"] = _gradients(grads, group.sizes, self.device)
+        o = DeflAdamwOpts()
+        o.beta1, o.beta2, o.eps, o.weight_decay = betas[0], betas[1], eps, weight_decay
+        if isinstance(lr, torch.Tensor):
+            o.lr_dev = self._scalar(lr, torch.float32, 1, "lr").data_ptr()
+        else:
+            o.lr = lr
+        if isinstance(step, torch.Tensor):
+            o.step_dev = self._scalar(step, torch.int64, 1, "step").data_ptr()
+        else:
+            o.step = step
+        if grad_scale is not None:
+            o.grad_scale = self._scalar(grad_scale, torch.float32, 2, "grad_scale").data_ptr() + 4
+        o.seed = seed
+        o.stochastic = int(bool(stochastic))
+        self._sync_stream()
+        self._check(lib().defl_adamw_step(self._h, table.ctypes.data, len(grads), ctypes.byref(o)))
+
+    def _scalar(self, t, dtype, count, what):
+        if t.device != self.device or t.dtype != dtype or t.numel() != count or not t.is_contiguous():
+            raise ValueError("%s must be a contiguous %s tensor of %d on %s" % (what, dtype, count, self.device))
+        return t
+
+    def defl_grad_norm(self, grads, max_norm=0.0, out=None, step=None):
+        """out[0] = the global norm of a list of gradients (None entries are skipped), out[1] = min(1, max_norm / (norm + 1e-6)),
+        or 0 if the norm is not finite; step, an int64 CUDA tensor [1], is advanced by one if it is finite. Nothing waits."""
+        out = torch.empty(2, dtype=torch.float32, device=self.device) if out is None else self._scalar(out, torch.float32, 2, "out")
+        grads = [g for g in grads if g is not None]
+        table = np.zeros(len(grads), dtype=_NORM_TENSOR)
+        if grads:
+            table["x"], table["dtype"] = _gradients(grads, None, self.device)
+            table["n"] = list(map(torch.Tensor.numel, grads))
+        if step is not None:
+            self._scalar(step, torch.int64, 1, "step")
+        work = torch.empty(int(lib().defl_grad_norm_work_bytes(len(grads))), dtype=torch.uint8, device=self.device)
+        self._sync_stream()
+        self._check(lib().defl_grad_norm(self._h, table.ctypes.data, len(grads), max_norm, out.data_ptr(),
+                                         step.data_ptr() if step is not None else None, work.data_ptr()))
+        return out
 
     def defl_fill_gaussian(self, dst, seed):
         _dev(dst, "dst")

@@ -1029,7 +1029,8 @@ int defl_muon_step_batched(defl_ctx* c, void* W, int w_dtype, void* Mom, const v
   const void* D = Mom;
   if (Grad) {
     void* look = nesterov ? c->stage_in : nullptr;
-    if (ctx_fail(c, momentum_launch(Mom, Grad, look, dtype, (long long)count, mu, c->stream, &c->launches), "momentum"))
+    if (ctx_fail(c, momentum_launch(Mom, Grad, look, dtype, (long long)count, mu, c->stream, &c->launches,
+                                     opts ? opts->grad_scale : nullptr), "momentum"))
       return DEFL_ERR_CUDA;
     if (nesterov) D = look;
   }

@@ -1369,9 +1369,14 @@ cudaError_t panel_pair_launch(const PanelPass& a, const PanelPass& b, int batch,
 // is given it receives Grad + mu Mom' with Mom' the STORED (rounded) new momentum, i.e. the Nesterov look-ahead
 // is a function of the optimizer state as it is kept in memory.
 // ---------------------------------------------------------------------------------------------
+// (a product of its own, not part of the fused multiply-add; a factor of zero drops gradients that are not finite)
+__device__ __forceinline__ float scaled_grad(float g, float c) { return c == 0.f ? 0.f : __fmul_rn(g, c); }
+
 template <typename T, int V>
-__global__ void __launch_bounds__(256) momentum_vec_kernel(T* Mom, const T* __restrict__ Grad, T* look, long long nvec, float mu) {
+__global__ void __launch_bounds__(256) momentum_vec_kernel(T* Mom, const T* __restrict__ Grad, T* look, long long nvec, float mu,
+                                                           const float* grad_scale) {
   pdl_wait();
+  const float c = grad_scale ? *grad_scale : 1.f;
   // V elements (16 bytes) per thread and trip
   struct alignas(16) Pack { T v[V]; };
   const long long stride = (long long)gridDim.x * blockDim.x;
@@ -1381,7 +1386,7 @@ __global__ void __launch_bounds__(256) momentum_vec_kernel(T* Mom, const T* __re
     Pack l;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const float gf = (float)g.v[j];
+      const float gf = scaled_grad((float)g.v[j], c);
       m.v[j] = (T)fmaf(mu, (float)m.v[j], gf);
       l.v[j] = (T)fmaf(mu, (float)m.v[j], gf);          // from the momentum as stored
     }
@@ -1391,17 +1396,18 @@ __global__ void __launch_bounds__(256) momentum_vec_kernel(T* Mom, const T* __re
 }
 
 __global__ void __launch_bounds__(256) momentum_kernel(void* Mom, const void* __restrict__ Grad, void* look, int dtype,
-                                                       long long first, long long count, float mu) {
+                                                       long long first, long long count, float mu, const float* grad_scale) {
   pdl_wait();
+  const float c = grad_scale ? *grad_scale : 1.f;
   const long long stride = (long long)gridDim.x * blockDim.x;
   for (long long i = first + (long long)blockIdx.x * blockDim.x + threadIdx.x; i < count; i += stride) {
-    const float g = ld_as_float(Grad, i, dtype);
+    const float g = scaled_grad(ld_as_float(Grad, i, dtype), c);
     st_from_float(Mom, i, dtype, fmaf(mu, ld_as_float(Mom, i, dtype), g));
     if (look) st_from_float(look, i, dtype, fmaf(mu, ld_as_float(Mom, i, dtype), g));
   }
 }
 cudaError_t momentum_launch(void* Mom, const void* Grad, void* look, int dtype, long long count, float mu, cudaStream_t st,
-                            long long* launches) {
+                            long long* launches, const float* grad_scale) {
   if (count <= 0) return cudaSuccess;
   const bool aligned = ((reinterpret_cast<uintptr_t>(Mom) | reinterpret_cast<uintptr_t>(Grad) | reinterpret_cast<uintptr_t>(look)) & 15) == 0;
   const int per = (dtype == BF16) ? 8 : 4;
@@ -1409,13 +1415,13 @@ cudaError_t momentum_launch(void* Mom, const void* Grad, void* look, int dtype, 
   if (nvec > 0) {
     const int nblk = (int)min((long long)148 * 16, (nvec + 255) / 256);
     if (dtype == BF16)
-      launch_kernel(momentum_vec_kernel<__nv_bfloat16, 8>, nblk, 256, 0, st, (__nv_bfloat16*)Mom, (const __nv_bfloat16*)Grad, (__nv_bfloat16*)look, nvec, mu);
+      launch_kernel(momentum_vec_kernel<__nv_bfloat16, 8>, nblk, 256, 0, st, (__nv_bfloat16*)Mom, (const __nv_bfloat16*)Grad, (__nv_bfloat16*)look, nvec, mu, grad_scale);
     else
-      launch_kernel(momentum_vec_kernel<float, 4>, nblk, 256, 0, st, (float*)Mom, (const float*)Grad, (float*)look, nvec, mu);
+      launch_kernel(momentum_vec_kernel<float, 4>, nblk, 256, 0, st, (float*)Mom, (const float*)Grad, (float*)look, nvec, mu, grad_scale);
     if (launches) ++*launches;
   }
   if (nvec * per < count) {      // the unaligned or leftover part
-    launch_kernel(momentum_kernel, 1, 256, 0, st, Mom, Grad, look, dtype, nvec * per, count, mu);
+    launch_kernel(momentum_kernel, 1, 256, 0, st, Mom, Grad, look, dtype, nvec * per, count, mu, grad_scale);
     if (launches) ++*launches;
   }
   return cudaGetLastError();

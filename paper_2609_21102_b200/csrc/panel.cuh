@@ -77,8 +77,8 @@ struct PanelPass {
 PanelPass panel_pass(const float* In, long long in_bs, int ld_in, int batch, int rows, int l, const float* Mtx, int ldm, int kout,
                      float* Out, long long out_bs, int ld_out, __nv_bfloat16* hi, __nv_bfloat16* lo, int lp, double* partial);
 cudaError_t panel_pair_launch(const PanelPass& a, const PanelPass& b, int batch, cudaStream_t st, long long* launches);
-// Muon momentum: Mom <- mu Mom + Grad (stored type `dtype`); look (may be null) <- Grad + mu Mom_stored
+// Muon momentum: Mom <- mu Mom + c Grad (stored type `dtype`); look (may be null) <- c Grad + mu Mom_stored; c = *grad_scale or 1
 cudaError_t momentum_launch(void* Mom, const void* Grad, void* look, int dtype, long long count, float mu, cudaStream_t st,
-                            long long* launches);
+                            long long* launches, const float* grad_scale);
 
 }  // namespace defl

@@ -374,6 +374,58 @@ typedef struct defl_norm_tensor {
 size_t defl_grad_norm_work_bytes(int count);
 int defl_grad_norm(defl_ctx* ctx, const defl_norm_tensor* tensors, int count, float max_norm, float* out, int64_t* step, void* work);
 
+/* ---- Microscaled 4-bit floating point --------------------------------------------------------------------------------
+ *
+ * A matrix [rows, cols] is held as e2m1 codes (0, .5, 1, 1.5, 2, 3, 4, 6 with a sign) with one scale per block of consecutive
+ * columns; a product contracts two such matrices along their columns, D = A B^T.
+ *   DEFL_MXFP4  blocks of 32; scale 2^e (a byte e + 127), the smallest power of two with largest magnitude <= 6 * 2^e
+ *   DEFL_NVFP4  blocks of 16; scale s * 2^w: w one number per matrix (held as scale = 2^w), the smallest with largest magnitude of the
+ *               matrix <= 6 * 448 * 2^w; s the e4m3 number nearest (ties to even) to the fp32 quotient (largest * 2^-w) / 6. The
+ *               matrix's scale is a power of two so that it costs no rounding; the products take any positive fp32 there.
+ * A code is the e2m1 number nearest to value / scale, ties to even. A block that holds Inf or NaN has a NaN for its scale (byte
+ * 255, or e4m3's 0x7f) and makes NaN of what it enters; the rest of the matrix is as if those values were zero.
+ * Layout, each matrix of a batch after the other:
+ *   codes   [rows, W / 2] bytes, W = cols rounded up to a multiple of 32 (the padding is zeros): columns 2j and 2j + 1 in the low and
+ *           the high half of byte j
+ *   scales  [ceil(rows / 128), ceil(blocks / 4), 512] bytes, blocks = W / 32 or W / 16: row r, block c of a tile of 128 rows x 4 blocks at
+ *           byte (r % 32) * 16 + (r / 32) * 4 + c, the order in which the tensor cores read them; padding is zeros
+ *   scale   [b] fp32 (DEFL_NVFP4; unused with DEFL_MXFP4)
+ * Buffers of codes and scales start on 16-byte boundaries; sides are at most DEFL_MX4_MAX_SIDE. */
+#define DEFL_MXFP4 0
+#define DEFL_NVFP4 1
+#define DEFL_MX4_MAX_SIDE (1 << 24)
+typedef struct defl_mx4 {
+  void* codes;
+  void* scales;
+  float* scale;
+} defl_mx4;
+size_t defl_mx4_codes_bytes(int b, int rows, int cols);
+size_t defl_mx4_scales_bytes(int b, int rows, int cols, int fmt);
+size_t defl_mx4_work_bytes(int b);
+
+/* Quantises X [b, rows, cols] (DEFL_BF16 or DEFL_F32; row stride ld >= cols and batch stride in elements), from one read (DEFL_NVFP4: a
+ * second one for the largest magnitude), into
+ *   by_rows  blocks along the columns of X: the matrix [rows, cols] as a product needs it that contracts cols; NULL: not wanted
+ *   by_cols  blocks along the rows of X: its transpose [cols, rows], for a product that contracts rows; NULL: not wanted
+ * A linear layer y = x w^T trains with x, w and dy in both directions: y = x w^T from by_rows of both, dx = dy w from dy's by_rows
+ * and w's by_cols, dw = dy^T x from both by_cols. (The gradient of the rounding itself is taken as one.)
+ *   work  device, defl_mx4_work_bytes(b) bytes, of this call alone until it is through; unused with DEFL_MXFP4 (may be NULL)
+ * Errors: DEFL_ERR_ARG, DEFL_ERR_RANK (a side above DEFL_MX4_MAX_SIDE, b above 65535), DEFL_ERR_CUDA. */
+int defl_mx4_quantize(defl_ctx* ctx, const void* X, int dtype, int b, int rows, int cols, int64_t ld, int64_t batch_stride, int fmt,
+                      const defl_mx4* by_rows, const defl_mx4* by_cols, void* work);
+
+/* out [b, rows, cols] contiguous, DEFL_BF16 or DEFL_F32: the values that the codes stand for, code * scale rounded once (both types
+ * hold them exactly while the matrix's scale is a power of two). */
+int defl_mx4_dequantize(defl_ctx* ctx, const defl_mx4* a, int b, int rows, int cols, int fmt, void* out, int dtype);
+
+/* D [b, M, N] = alpha A B^T with A [b, M, K] and B [b, N, K], or one B for all (b_shared != 0), of the same format; D row-major with row
+ * stride ldd >= N and a batch stride of its own, DEFL_BF16 or DEFL_F32. Products are exact, sums are fp32, one rounding to bf16.
+ * Up to eight rows of A (single tokens) the weights stream through integer products, else the tensor cores take the
+ * scales with the codes (tcgen05 block-scaled products). A device-side wait that runs out is reported by
+ * defl_device_wait_status. Errors as defl_mx4_quantize. */
+int defl_mx4_gemm(defl_ctx* ctx, const defl_mx4* A, const defl_mx4* B, int b, int M, int N, int K, int b_shared, int fmt, float alpha, void* D,
+                  int64_t ldd, int64_t batch_stride, int out_dtype);
+
 /* Diagnostics: one batched product C[b,M,N] = alpha * opA(A) opB(B) through a chosen engine, used by the
  * tests to check the tensor-core tile engine against the fp32 engine (no counterpart in the paper).
  * A element (i,kk) is A[i*sa_i + kk*sa_k], B element (kk,j) is B[kk*sb_k + j*sb_j]; C is row-major [M,N].

@@ -8,6 +8,7 @@ CUDA kernels. There is no fallback: if the shared library is missing the import 
 import ctypes
 import operator
 import os
+from typing import NamedTuple, Optional
 
 import numpy as np
 import torch
@@ -21,6 +22,7 @@ NORM_LANCZOS, NORM_FROBENIUS = 0, 1
 ENGINE_AUTO, ENGINE_SIMT, ENGINE_TENSOR = 0, 1, 2
 ST_CHOL_SHIFT, ST_JACOBI_CAP, ST_ZERO_RESIDUAL, ST_DEVICE_WAIT, ST_NONFINITE = 1, 2, 4, 8, 16
 MAX_L, MAX_STEPS, MAX_TERMS = 64, 32, 6
+MX4_FORMATS = {"mxfp4": 0, "nvfp4": 1}
 
 MUON_QUINTIC = (3.4445, -4.7750, 2.0315)
 CLASSICAL_QUINTIC = (1.875, -1.25, 0.375)
@@ -30,6 +32,7 @@ EXPORTS = [
     "defl_polar_window", "defl_psd_window", "defl_polar_batched", "defl_polar_batched_host", "defl_muon_step_batched", "defl_brsvd_batched", "defl_psd_project", "defl_inv_root", "defl_admm_diag_sdp", "defl_fill_gaussian", "defl_debug_gemm",
     "defl_frobenius_norms_noalloc", "defl_set_profiling", "defl_get_stage_ms", "defl_get_stage_ms_sum", "defl_launch_count", "defl_device_wait_status",
     "defl_status_string", "defl_last_error", "defl_adamw_step", "defl_grad_norm", "defl_grad_norm_work_bytes",
+    "defl_mx4_codes_bytes", "defl_mx4_scales_bytes", "defl_mx4_work_bytes", "defl_mx4_quantize", "defl_mx4_dequantize", "defl_mx4_gemm",
 ]
 
 
@@ -45,6 +48,10 @@ class DeflAdamwOpts(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
                 ("weight_decay", ctypes.c_double), ("step", ctypes.c_int64), ("step_dev", ctypes.c_void_p), ("lr_dev", ctypes.c_void_p),
                 ("grad_scale", ctypes.c_void_p), ("seed", ctypes.c_uint64), ("stochastic", ctypes.c_int)]
+
+
+class DeflMx4(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
 
 
 # the tables of defl_adamw_tensor and defl_norm_tensor entries, laid out as the C compiler does
@@ -105,6 +112,16 @@ def lib():
         L.defl_grad_norm_work_bytes.restype = ctypes.c_size_t
         L.defl_grad_norm_work_bytes.argtypes = [ctypes.c_int]
         L.defl_grad_norm.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_float] + [ctypes.c_void_p] * 3
+        L.defl_mx4_codes_bytes.restype = L.defl_mx4_scales_bytes.restype = L.defl_mx4_work_bytes.restype = ctypes.c_size_t
+        L.defl_mx4_codes_bytes.argtypes = [ctypes.c_int] * 3
+        L.defl_mx4_scales_bytes.argtypes = [ctypes.c_int] * 4
+        L.defl_mx4_work_bytes.argtypes = [ctypes.c_int]
+        L.defl_mx4_quantize.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                        ctypes.c_int64, ctypes.c_int64, ctypes.c_int, ctypes.POINTER(DeflMx4), ctypes.POINTER(DeflMx4),
+                                        ctypes.c_void_p]
+        L.defl_mx4_dequantize.argtypes = [ctypes.c_void_p, ctypes.POINTER(DeflMx4)] + [ctypes.c_int] * 4 + [ctypes.c_void_p, ctypes.c_int]
+        L.defl_mx4_gemm.argtypes = [ctypes.c_void_p, ctypes.POINTER(DeflMx4), ctypes.POINTER(DeflMx4)] + [ctypes.c_int] * 6 + [
+            ctypes.c_float, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64, ctypes.c_int]
         L.defl_set_profiling.argtypes = [ctypes.c_void_p, ctypes.c_int]
         L.defl_get_stage_ms.argtypes = [ctypes.c_void_p, ctypes.POINTER(ctypes.c_float), ctypes.c_int]
         L.defl_get_stage_ms_sum.argtypes = [ctypes.c_void_p, ctypes.POINTER(ctypes.c_float), ctypes.c_int, ctypes.c_int]
@@ -174,6 +191,31 @@ def defl_psd_window(n, w, w_prime):
     if rc != 0:
         raise DeflError(rc)
     return k.value, K.value
+
+
+class Mx4(NamedTuple):
+    """A batch of matrices [rows, cols] in microscaled 4-bit floating point, blocks along cols (layout: include/defl.h).
+    codes uint8 [b, rows, W / 2], W = cols rounded up to 32; scales uint8 [b, ceil(rows / 128), ceil(blocks / 4), 512]; scale float32
+    [b] (nvfp4; unused with mxfp4); fmt "mxfp4" or "nvfp4"."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    scale: Optional[torch.Tensor]
+    fmt: str
+    rows: int
+    cols: int
+
+    def plain_scales(self):
+        """The scale bytes in rows, uint8 [b, rows, blocks] (a copy)."""
+        b, rt, kt, _ = self.scales.shape
+        t = self.scales.view(b, rt, kt, 32, 4, 4).permute(0, 1, 4, 3, 2, 5).reshape(b, rt * 128, kt * 4)
+        return t[:, :self.rows, :(self.cols + 31) // 32 * (1 if self.fmt == "mxfp4" else 2)]
+
+
+def _mx4_shapes(b, rows, cols, fmt):
+    """Shapes of codes and scales."""
+    width = (cols + 31) // 32 * 32
+    per = 128 if fmt == "mxfp4" else 64
+    return (b, rows, width // 2), (b, (rows + 127) // 128, (width + per - 1) // per, 512)
 
 
 def _gradients(grads, sizes, device):
@@ -535,6 +577,79 @@ class Context:
         self._sync_stream()
         self._check(lib().defl_grad_norm(self._h, table.ctypes.data, len(grads), max_norm, out.data_ptr(),
                                          step.data_ptr() if step is not None else None, work.data_ptr()))
+        return out
+
+    def _mx4_new(self, b, rows, cols, fmt):
+        codes, scales = _mx4_shapes(b, rows, cols, fmt)
+        return Mx4(torch.empty(codes, dtype=torch.uint8, device=self.device), torch.empty(scales, dtype=torch.uint8, device=self.device),
+                   torch.empty(b, dtype=torch.float32, device=self.device) if fmt == "nvfp4" else None, fmt, rows, cols)
+
+    def _mx4_ref(self, q, what):
+        if q.fmt not in MX4_FORMATS:
+            raise ValueError("%s: the format is mxfp4 or nvfp4, got %r" % (what, q.fmt))
+        codes, scales = _mx4_shapes(q.codes.shape[0], q.rows, q.cols, q.fmt)
+        for t, shape in ((q.codes, codes), (q.scales, scales)):
+            if t.device != self.device or t.dtype != torch.uint8 or tuple(t.shape) != shape or not t.is_contiguous():
+                raise ValueError("%s must hold contiguous uint8 tensors of shapes %s and %s on %s" % (what, codes, scales, self.device))
+        r = DeflMx4(q.codes.data_ptr(), q.scales.data_ptr(), None)
+        if q.fmt == "nvfp4":
+            if q.scale is None:
+                raise ValueError("%s needs its matrices' scales" % what)
+            r.scale = self._scalar(q.scale, torch.float32, codes[0], what + ".scale").data_ptr()
+        return r
+
+    def defl_mx4_quantize(self, X, fmt="mxfp4", transposed=False, both=False):
+        """X [b, rows, cols] (bfloat16 or float32; one of the last two strides is 1) to 4 bits: blocks along cols, an Mx4 of [rows, cols];
+        `transposed`: blocks along rows, an Mx4 of the transpose [cols, rows]; `both`: a pair of them from one read."""
+        if fmt not in MX4_FORMATS:
+            raise ValueError("the format is mxfp4 or nvfp4, got %r" % (fmt,))
+        if X.ndim != 3 or X.device != self.device or X.dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError("X must be a bfloat16 or float32 tensor [b, rows, cols] on %s" % self.device)
+        b, rows, cols = X.shape
+        want = (both or not transposed, both or transposed)
+        made = tuple(self._mx4_new(b, *((rows, cols) if i == 0 else (cols, rows)), fmt) if want[i] else None for i in (0, 1))
+        batch, sr, sc = X.stride()
+        order = made
+        if cols > 1 and sc != 1:
+            if rows > 1 and sr != 1:
+                raise ValueError("one of X's last two dimensions must be contiguous")
+            rows, cols, sr, order = cols, rows, sc, (made[1], made[0])     # the same matrices, seen from the other side
+        if rows == 1:
+            sr = cols
+        if sr < cols or batch < 0:
+            raise ValueError("X's rows overlap or run backwards")
+        refs = [ctypes.byref(self._mx4_ref(q, "result")) if q is not None else None for q in order]
+        work = None
+        if fmt == "nvfp4" and rows * cols > 32768:
+            work = torch.empty(int(lib().defl_mx4_work_bytes(b)), dtype=torch.uint8, device=self.device)
+        self._sync_stream()
+        self._check(lib().defl_mx4_quantize(self._h, X.data_ptr(), _dtype_code(X), b, rows, cols, sr, batch, MX4_FORMATS[fmt], refs[0],
+                                            refs[1], work.data_ptr() if work is not None else None))
+        return made if both else made[1] if transposed else made[0]
+
+    def defl_mx4_dequantize(self, q, dtype=torch.bfloat16):
+        """The values [b, rows, cols] that an Mx4 stands for."""
+        ref = self._mx4_ref(q, "q")
+        out = torch.empty((q.codes.shape[0], q.rows, q.cols), dtype=dtype, device=self.device)
+        self._sync_stream()
+        self._check(lib().defl_mx4_dequantize(self._h, ctypes.byref(ref), q.codes.shape[0], q.rows, q.cols, MX4_FORMATS[q.fmt], out.data_ptr(),
+                                              _dtype_code(out)))
+        return out
+
+    def defl_mx4_gemm(self, A, B, out_dtype=torch.bfloat16, out=None, alpha=1.0):
+        """alpha A B^T [b, M, N] of two Mx4 of one format that agree in cols; a B of batch 1 serves every A."""
+        ra, rb = self._mx4_ref(A, "A"), self._mx4_ref(B, "B")
+        b = A.codes.shape[0]
+        if A.fmt != B.fmt or A.cols != B.cols or B.codes.shape[0] not in (1, b):
+            raise ValueError("A and B must agree in format, columns and batch")
+        if out is None:
+            out = torch.empty((b, A.rows, B.rows), dtype=out_dtype, device=self.device)
+        elif out.device != self.device or tuple(out.shape) != (b, A.rows, B.rows) or (B.rows > 1 and out.stride(2) != 1):
+            raise ValueError("out must be [b, M, N] on %s with contiguous rows" % self.device)
+        ld = out.stride(1) if A.rows > 1 else B.rows
+        self._sync_stream()
+        self._check(lib().defl_mx4_gemm(self._h, ctypes.byref(ra), ctypes.byref(rb), b, A.rows, B.rows, A.cols, int(B.codes.shape[0] == 1),
+                                        MX4_FORMATS[A.fmt], alpha, out.data_ptr(), ld, out.stride(0), _dtype_code(out)))
         return out
 
     def defl_fill_gaussian(self, dst, seed):

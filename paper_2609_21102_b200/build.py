@@ -6,7 +6,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdeflpolar.so")
-SOURCES = ["api.cu", "psd.cu", "gemm_simt.cu", "gemm_tc.cu", "panel.cu", "optim.cu"]
+SOURCES = ["api.cu", "psd.cu", "gemm_simt.cu", "gemm_tc.cu", "panel.cu", "optim.cu", "mx4.cu", "mx4_gemm.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "--use_fast_math=false"]
 

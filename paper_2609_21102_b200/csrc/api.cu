@@ -4,6 +4,7 @@
 #include "../../include/defl.h"
 #include "common.cuh"
 #include "panel.cuh"
+#include "mx4.cuh"
 #include "ctx.cuh"
 #include <cstdlib>
 
@@ -335,7 +336,8 @@ int defl_create(defl_ctx** out, int device) {
   c->knobs.lanczos_form = getenv("DEFL_LANCZOS_FORM") ? atoi(getenv("DEFL_LANCZOS_FORM")) : 0;
   c->knobs.lanczos_hold = getenv("DEFL_LANCZOS_HOLD") ? 1 : 0;
   cudaDeviceGetAttribute(&c->num_sms, cudaDevAttrMultiProcessorCount, device);
-  int ok = gemm_tc_prepare() == cudaSuccess && panel_prepare() == cudaSuccess && psd_prepare() == cudaSuccess ? 1 : 0;
+  int ok = gemm_tc_prepare() == cudaSuccess && panel_prepare() == cudaSuccess && psd_prepare() == cudaSuccess &&
+           mx4_quantize_prepare() == cudaSuccess && mx4_gemm_prepare() == cudaSuccess ? 1 : 0;
   if (ok && cudaMalloc(&c->wait_status, 2 * sizeof(int)) != cudaSuccess) ok = 0;      // status word, tile counter
   if (ok) cudaMemset(c->wait_status, 0, 2 * sizeof(int));
   if (ok) {

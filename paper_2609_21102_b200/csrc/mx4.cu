@@ -1,0 +1,498 @@
+// Microscaled 4-bit floating point: quantisation in one or both block directions from one read, the way back, and the
+// products' entry point. Definitions and layout are in include/defl.h.
+#include "../../include/defl.h"
+#include "ctx.cuh"
+#include "mx4.cuh"
+#include <cuda_fp8.h>
+#include <math.h>
+#include <type_traits>
+
+namespace defl {
+namespace {
+
+constexpr int TILE = 128;                  // a CTA takes 128 x 128 values: a whole tile of scales in either direction
+constexpr int Q_THREADS = 256;
+constexpr int MAX_PARTIALS = 592;          // partial maxima a call (four CTAs an SM), at least one a matrix
+constexpr int SCAN_MOST = 32768;           // matrices up to this size: every CTA finds the largest magnitude by itself
+
+struct QuantParams {
+  const void* X;
+  long long ld, batch_stride;
+  int b, rows, cols;
+  int tiles_c;
+  uint8_t* rc; uint8_t* rs; float* rscale;     // blocks along the rows (null: not wanted)
+  uint8_t* cc; uint8_t* cs; float* cscale;     // blocks along the columns
+  const float* partial;                        // largest finite magnitudes of parts of each matrix (nvfp4)
+  int nper;                                    // partial maxima a matrix; 0: the matrix is small, look at it here
+};
+
+template <typename T> __device__ __forceinline__ uint32_t magnitude_bits(T x);           // as those of a float
+template <> __device__ __forceinline__ uint32_t magnitude_bits<float>(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+template <> __device__ __forceinline__ uint32_t magnitude_bits<__nv_bfloat16>(__nv_bfloat16 x) {
+  return ((uint32_t)__bfloat16_as_ushort(x) & 0x7fffu) << 16;
+}
+__device__ __forceinline__ uint32_t finite_or_zero(uint32_t bits) { return bits < 0x7f800000u ? bits : 0u; }
+
+// Eight values to eight e2m1 codes, the first in the low bits: to nearest, ties to even, magnitudes above 6 to 6.
+__device__ __forceinline__ uint32_t e2m1x8(const float* v) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+      "mov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(r) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+  return r;
+}
+
+// exponent byte of the power of two of an nvfp4 matrix whose largest magnitude has these bits: the smallest with
+// largest <= 448 * 6 * 2^w (2688 = 1.3125 * 2^11), at least 2^-126; 1 for a matrix of zeros
+__device__ __forceinline__ int whole_exponent(uint32_t top) {
+  if (top == 0u) return 127;
+  const int e = (int)((top + 0x57ffffu) >> 23) - 11;
+  return e > 1 ? e : 1;
+}
+
+// What a block's values are multiplied by, and its scale byte.
+struct BlockScale {
+  float pre, r, s;        // mxfp4: value * r. nvfp4: value * pre / s, r = 1 / s
+  uint32_t byte;
+};
+template <int FMT>
+__device__ __forceinline__ BlockScale block_scale(uint32_t big, float pre) {
+  BlockScale q;
+  q.pre = pre;
+  if (FMT == MXFP4) {
+    // the smallest power of two with big <= 6 * 2^e = 1.5 * 2^(e + 2). (The usual rule 2^(floor(log2 big) - 2) clips whatever
+    // lies above 6 of 8, up to a quarter of the block's largest value.)
+    const int byte = (int)((big + 0x3fffffu) >> 23) - 2;
+    q.byte = byte > 0 ? (uint32_t)byte : 0u;
+    q.r = __uint_as_float((254u - q.byte) << 23);
+    q.s = 0.f;
+    if (big >= 0x7f800000u) q.byte = 255u;                    // NaN: Inf and NaN have no place in a block
+  } else {
+    const float a = __fdiv_rn(__uint_as_float(big) * pre, 6.f);
+    q.byte = (uint32_t)__nv_cvt_float_to_fp8(a, __NV_SATFINITE, __NV_E4M3);
+    q.s = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)q.byte, __NV_E4M3)));
+    q.r = q.s > 0.f ? __frcp_rn(q.s) : 0.f;
+    if (big >= 0x7f800000u) q.byte = 0x7fu;
+  }
+  return q;
+}
+// The quotient x * pre / s correctly rounded: the product with the rounded reciprocal, and one correction by its exact
+// remainder (Markstein 1990). The plain product would miss the ties between two codes, which values of few bits often hit.
+template <int FMT>
+__device__ __forceinline__ float scaled(float x, const BlockScale& q) {
+  if (FMT == MXFP4) return x * q.r;
+  const float y = x * q.pre, a = y * q.r;
+  return fmaf(fmaf(-a, q.s, y), q.r, a);
+}
+
+// Where a row of the tile starts in shared memory, in words: rows of 32 columns further on are shifted by 8 words, so that the
+// column pass (four row blocks x eight columns a warp) meets no bank twice.
+template <typename T> __device__ __forceinline__ int row_word(int r) { return r * (TILE * (int)sizeof(T) / 4) + 8 * (r >> 5); }
+template <typename T> __host__ __device__ constexpr int tile_bytes() { return (TILE * TILE * (int)sizeof(T) / 4 + 32) * 4; }
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+// Reads 2 or 4 bytes a value and writes half a byte and 1/32 or 1/16 a direction: bound by HBM, which leaves some fifteen
+// instructions a value. The tile goes through shared memory once; both passes read it from there.
+template <typename T, int FMT, bool VEC>
+__global__ void __launch_bounds__(Q_THREADS) mx4_quantize_kernel(const QuantParams p) {
+  constexpr int BLK = FMT == MXFP4 ? 32 : 16, SBYTES = TILE / BLK * TILE, ES = (int)sizeof(T);
+  extern __shared__ __align__(16) uint8_t smem[];
+  uint8_t* const s_row = smem + tile_bytes<T>();
+  uint8_t* const s_col = s_row + SBYTES;
+  __shared__ uint32_t s_top[Q_THREADS / 32];
+  uint32_t* const words = reinterpret_cast<uint32_t*>(smem);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int bz = blockIdx.y;
+  const int tr = (int)(blockIdx.x / (unsigned)p.tiles_c), tc = (int)(blockIdx.x - (unsigned)tr * (unsigned)p.tiles_c);
+  const int row0 = tr * TILE, col0 = tc * TILE;
+  const T* const X = reinterpret_cast<const T*>(p.X) + (long long)bz * p.batch_stride;
+  pdl_wait();
+  if (VEC) {
+    constexpr int PER = TILE * ES / 16;          // 16-byte pieces a row
+    const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem);
+#pragma unroll
+    for (int i = 0; i < TILE * PER / Q_THREADS; ++i) {
+      const int u = tid + Q_THREADS * i, r = u / PER, c = (u % PER) * (16 / ES);
+      int left = row0 + r < p.rows ? (p.cols - col0 - c) * ES : 0;
+      left = left < 0 ? 0 : left > 16 ? 16 : left;
+      copy16(base + 4 * row_word<T>(r) + (u % PER) * 16, left ? X + (long long)(row0 + r) * p.ld + col0 + c : X, (uint32_t)left);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  } else {
+#pragma unroll 16
+    for (int i = 0; i < TILE * TILE / Q_THREADS; ++i) {
+      const int u = tid + Q_THREADS * i, r = u / TILE, c = u % TILE;
+      const bool on = row0 + r < p.rows && col0 + c < p.cols;
+      const T x = on ? X[(long long)(row0 + r) * p.ld + col0 + c] : (T)0.f;
+      reinterpret_cast<T*>(words + row_word<T>(r))[c] = x;
+    }
+  }
+  float pre = 1.f;
+  if (FMT == NVFP4) {
+    uint32_t top = 0;
+    if (p.nper > 0) {
+      for (int i = tid; i < p.nper; i += Q_THREADS) top = max(top, __float_as_uint(p.partial[(long long)bz * p.nper + i]));
+    } else {
+      for (int u = tid; u < p.rows * p.cols; u += Q_THREADS) {
+        const int r = u / p.cols;
+        top = max(top, finite_or_zero(magnitude_bits(X[(long long)r * p.ld + (u - r * p.cols)])));
+      }
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    if (lane == 0) s_top[warp] = top;
+  }
+  if (VEC) asm volatile("cp.async.wait_group 0;" ::: "memory");
+  __syncthreads();
+  if (FMT == NVFP4) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < Q_THREADS / 32; ++i) top = max(top, s_top[i]);
+    const int e = whole_exponent(top);
+    pre = __uint_as_float((uint32_t)(254 - e) << 23);
+    if (blockIdx.x == 0 && tid == 0) {
+      const float whole = __uint_as_float((uint32_t)e << 23);
+      if (p.rscale) p.rscale[bz] = whole;
+      if (p.cscale) p.cscale[bz] = whole;
+    }
+  }
+
+  if (p.rc) {
+    const int width = mx4_width(p.cols);
+    uint8_t* const out = p.rc + (long long)bz * p.rows * (width / 2);
+#pragma unroll 4
+    for (int i = 0; i < TILE * TILE / 8 / Q_THREADS; ++i) {
+      const int u = tid + Q_THREADS * i, r = u >> 4, c8 = u & 15;
+      float v[8];
+      uint32_t big = 0;
+      if (ES == 2) {
+        const uint4 q = *reinterpret_cast<const uint4*>(words + row_word<T>(r) + 4 * c8);
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          big = __vmaxu2(big, w[j] & 0x7fff7fffu);
+          v[2 * j] = __uint_as_float(w[j] << 16);
+          v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+        }
+#pragma unroll
+        for (int o = 1; o < BLK / 8; o <<= 1) big = __vmaxu2(big, __shfl_xor_sync(0xffffffffu, big, o));
+        big = max(big << 16, big & 0xffff0000u);
+      } else {
+        const float4* f = reinterpret_cast<const float4*>(words + row_word<T>(r) + 8 * c8);
+        const float4 a = f[0], b = f[1];
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) big = max(big, magnitude_bits(v[j]));
+#pragma unroll
+        for (int o = 1; o < BLK / 8; o <<= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
+      }
+      const BlockScale q = block_scale<FMT>(big, pre);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = scaled<FMT>(v[j], q);
+      const uint32_t codes = e2m1x8(v);
+      if (row0 + r < p.rows && col0 + 8 * c8 < width)
+        *reinterpret_cast<uint32_t*>(out + (long long)(row0 + r) * (width / 2) + (col0 + 8 * c8) / 2) = codes;
+      if (c8 % (BLK / 8) == 0) {
+        const int blk = c8 / (BLK / 8);
+        s_row[(blk >> 2) * 512 + (r & 31) * 16 + (r >> 5) * 4 + (blk & 3)] = (uint8_t)q.byte;
+      }
+    }
+  }
+
+  if (p.cc) {
+    const int width = mx4_width(p.rows);         // codes a column
+    uint8_t* const out = p.cc + (long long)bz * p.cols * (width / 2);
+    const int rb = lane & 3;                     // rows 32 rb ..
+    constexpr int COLS = ES == 2 ? 2 : 1;        // columns of a word
+#pragma unroll 1
+    for (int i = 0; i < 2 / COLS; ++i) {
+      const int cw = (lane >> 2) + 8 * warp + 64 * i;
+      uint32_t w[32];
+#pragma unroll
+      for (int j = 0; j < 32; ++j) w[j] = words[row_word<T>(32 * rb) + j * (TILE * ES / 4) + cw];
+#pragma unroll
+      for (int k = 0; k < COLS; ++k) {
+        const int c = cw * COLS + k;
+        uint32_t codes[4];
+#pragma unroll
+        for (int h = 0; h < 32 / BLK; ++h) {
+          uint32_t big = 0;
+#pragma unroll
+          for (int j = 0; j < BLK; ++j) {
+            const uint32_t x = ES == 4 ? w[BLK * h + j] & 0x7fffffffu : (k == 0 ? w[BLK * h + j] << 16 : w[BLK * h + j]) & 0x7fff0000u;
+            big = max(big, x);
+          }
+          const BlockScale q = block_scale<FMT>(big, pre);
+#pragma unroll
+          for (int o = 0; o < BLK / 8; ++o) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const uint32_t x = w[BLK * h + 8 * o + j];
+              v[j] = scaled<FMT>(__uint_as_float(ES == 4 ? x : k == 0 ? x << 16 : x & 0xffff0000u), q);
+            }
+            codes[(BLK / 8) * h + o] = e2m1x8(v);
+          }
+          const int blk = rb * (32 / BLK) + h;
+          s_col[(blk >> 2) * 512 + (c & 31) * 16 + (c >> 5) * 4 + (blk & 3)] = (uint8_t)q.byte;
+        }
+        if (col0 + c < p.cols && row0 + 32 * rb < width)
+          *reinterpret_cast<uint4*>(out + (long long)(col0 + c) * (width / 2) + (row0 + 32 * rb) / 2) = make_uint4(codes[0], codes[1], codes[2], codes[3]);
+      }
+    }
+  }
+
+  __syncthreads();
+  // the tiles of scales, whole: rows and blocks that do not exist have zeros
+  constexpr int NT = SBYTES / 512;
+  if (p.rc) {
+    const int kt = mx4_scale_tiles(p.cols, FMT), first = tc * NT;
+    if (tid * 4 < min(NT, kt - first) * 512)
+      reinterpret_cast<uint32_t*>(p.rs + (((long long)bz * mx4_row_tiles(p.rows) + tr) * kt + first) * 512)[tid] = reinterpret_cast<uint32_t*>(s_row)[tid];
+  }
+  if (p.cc) {
+    const int kt = mx4_scale_tiles(p.rows, FMT), first = tr * NT;
+    if (tid * 4 < min(NT, kt - first) * 512)
+      reinterpret_cast<uint32_t*>(p.cs + (((long long)bz * mx4_row_tiles(p.cols) + tc) * kt + first) * 512)[tid] = reinterpret_cast<uint32_t*>(s_col)[tid];
+  }
+}
+
+// Largest finite magnitude of a part of each matrix (nvfp4): rows are dealt to the CTAs of a matrix.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(Q_THREADS) mx4_amax_kernel(const void* Xv, long long ld, long long batch_stride, int rows, int cols, float* partial) {
+  __shared__ uint32_t s_top[Q_THREADS / 32];
+  pdl_wait();
+  const T* const X = reinterpret_cast<const T*>(Xv) + (long long)blockIdx.y * batch_stride;
+  constexpr int V = 16 / (int)sizeof(T);
+  const long long per = VEC ? (cols + V - 1) / V : cols, count = per * rows, step = (long long)gridDim.x * Q_THREADS;
+  uint32_t top = 0;
+  // (row and column are carried along: the step is a fixed number of rows and columns)
+  const long long u0 = (long long)blockIdx.x * Q_THREADS + threadIdx.x;
+  long long r = u0 / per, c = u0 - r * per;
+  const long long dr = step / per, dc = step - dr * per;
+#pragma unroll 4
+  for (long long u = u0; u < count; u += step) {
+    if (VEC && c * V + V <= cols) {
+      const uint4 q = *reinterpret_cast<const uint4*>(X + r * ld + c * V);
+      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (sizeof(T) == 4) top = max(top, finite_or_zero(w[j] & 0x7fffffffu));
+        else top = max(top, max(finite_or_zero((w[j] << 16) & 0x7fff0000u), finite_or_zero(w[j] & 0x7fff0000u)));
+      }
+    } else {
+      const int n = VEC ? V : 1;
+      for (int j = 0; j < n; ++j)
+        if (c * n + j < cols) top = max(top, finite_or_zero(magnitude_bits(X[r * ld + c * n + j])));
+    }
+    r += dr; c += dc;
+    if (c >= per) { c -= per; ++r; }
+  }
+  top = __reduce_max_sync(0xffffffffu, top);
+  if ((threadIdx.x & 31) == 0) s_top[threadIdx.x >> 5] = top;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < Q_THREADS / 32; ++i) top = max(top, s_top[i]);
+    partial[(long long)blockIdx.y * gridDim.x + blockIdx.x] = __uint_as_float(top);
+  }
+}
+
+__device__ __forceinline__ float2 e2m1x2(uint32_t two) {
+  uint32_t h;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\t}" : "=r"(h) : "r"(two));
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+
+// A warp a row; eight values a lane and trip. Bound by HBM: half a byte in, 2 or 4 out.
+template <int FMT, typename O>
+__global__ void __launch_bounds__(Q_THREADS) mx4_dequantize_kernel(Mx4View a, int b, int rows, int cols, O* out, int vec) {
+  constexpr int BLK = FMT == MXFP4 ? 32 : 16;
+  pdl_wait();
+  const long long id = (long long)blockIdx.x * (Q_THREADS / 32) + (threadIdx.x >> 5);
+  if (id >= (long long)b * rows) return;
+  const int lane = threadIdx.x & 31, bz = (int)(id / rows), r = (int)(id - (long long)bz * rows);
+  const int width = mx4_width(cols), kt = mx4_scale_tiles(cols, FMT);
+  const uint32_t* const codes = reinterpret_cast<const uint32_t*>(a.codes + id * (width / 2));
+  const uint8_t* const sc = a.scales + ((long long)bz * mx4_row_tiles(rows) + (r >> 7)) * kt * 512 + (r & 31) * 16 + ((r >> 5) & 3) * 4;
+  const float whole = FMT == NVFP4 ? a.scale[bz] : 1.f;
+  O* const dst = out + id * cols;
+#pragma unroll 4
+  for (int c8 = lane; c8 * 8 < cols; c8 += 32) {
+    const uint32_t q = codes[c8];
+    const int blk = c8 * 8 / BLK;
+    const uint32_t byte = sc[(long long)(blk >> 2) * 512 + (blk & 3)];
+    float s;
+    if (FMT == MXFP4) s = byte == 255u ? __uint_as_float(0x7fffffffu) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
+    else s = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)byte, __NV_E4M3))) * whole;
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 f = e2m1x2(q >> (8 * j));
+      v[2 * j] = f.x * s; v[2 * j + 1] = f.y * s;
+    }
+    if (vec) {
+      if (sizeof(O) == 2) {
+        *reinterpret_cast<uint4*>(dst + 8 * c8) = make_uint4(pack16x2(v[0], v[1], false), pack16x2(v[2], v[3], false), pack16x2(v[4], v[5], false), pack16x2(v[6], v[7], false));
+      } else {
+        reinterpret_cast<float4*>(dst + 8 * c8)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(dst + 8 * c8)[1] = make_float4(v[4], v[5], v[6], v[7]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (8 * c8 + j < cols) dst[8 * c8 + j] = (O)v[j];
+    }
+  }
+}
+
+template <typename T, int FMT>
+constexpr int quantize_smem() { return tile_bytes<T>() + 2 * (TILE / (FMT == MXFP4 ? 32 : 16) * TILE); }
+
+template <typename T, int FMT>
+cudaError_t quantize_launch(const QuantParams& p, bool vec, cudaStream_t st) {
+  const dim3 grid((unsigned)p.tiles_c * (unsigned)((p.rows + TILE - 1) / TILE), (unsigned)p.b);
+  return vec ? launch_kernel(mx4_quantize_kernel<T, FMT, true>, grid, dim3(Q_THREADS), quantize_smem<T, FMT>(), st, p)
+             : launch_kernel(mx4_quantize_kernel<T, FMT, false>, grid, dim3(Q_THREADS), quantize_smem<T, FMT>(), st, p);
+}
+template <typename T>
+cudaError_t amax_launch(const void* X, long long ld, long long batch_stride, int rows, int cols, int b, int nper, float* partial, bool vec, cudaStream_t st) {
+  const dim3 grid((unsigned)nper, (unsigned)b);
+  return vec ? launch_kernel(mx4_amax_kernel<T, true>, grid, dim3(Q_THREADS), 0, st, X, ld, batch_stride, rows, cols, partial)
+             : launch_kernel(mx4_amax_kernel<T, false>, grid, dim3(Q_THREADS), 0, st, X, ld, batch_stride, rows, cols, partial);
+}
+template <typename T, int FMT>
+cudaError_t quantize_limit() {
+  cudaError_t e = cudaFuncSetAttribute(mx4_quantize_kernel<T, FMT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, quantize_smem<T, FMT>());
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(mx4_quantize_kernel<T, FMT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, quantize_smem<T, FMT>());
+}
+
+bool on(const void* p, unsigned a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+struct DeviceScope {
+  int prev = 0;
+  explicit DeviceScope(int dev) {
+    cudaGetDevice(&prev);
+    if (prev != dev) cudaSetDevice(dev); else prev = -1;
+  }
+  ~DeviceScope() { if (prev >= 0) cudaSetDevice(prev); }
+};
+
+int partials_of(int b) { return b >= MAX_PARTIALS ? 1 : MAX_PARTIALS / b; }
+
+bool matrix_ok(const defl_mx4* m, int fmt) {
+  return m->codes && m->scales && on(m->codes, 16) && on(m->scales, 16) && (fmt == DEFL_MXFP4 || m->scale);
+}
+
+}  // namespace
+
+cudaError_t mx4_quantize_prepare() {
+  cudaError_t e;
+  if ((e = quantize_limit<float, MXFP4>()) != cudaSuccess) return e;
+  if ((e = quantize_limit<float, NVFP4>()) != cudaSuccess) return e;
+  if ((e = quantize_limit<__nv_bfloat16, MXFP4>()) != cudaSuccess) return e;
+  return quantize_limit<__nv_bfloat16, NVFP4>();
+}
+
+}  // namespace defl
+
+using namespace defl;
+
+extern "C" {
+
+size_t defl_mx4_codes_bytes(int b, int rows, int cols) {
+  return b <= 0 || rows <= 0 || cols <= 0 ? 0 : (size_t)b * rows * (mx4_width(cols) / 2);
+}
+size_t defl_mx4_scales_bytes(int b, int rows, int cols, int fmt) {
+  if (b <= 0 || rows <= 0 || cols <= 0 || (fmt != DEFL_MXFP4 && fmt != DEFL_NVFP4)) return 0;
+  return (size_t)b * mx4_row_tiles(rows) * mx4_scale_tiles(cols, fmt) * 512;
+}
+size_t defl_mx4_work_bytes(int b) { return b <= 0 ? 0 : (size_t)b * partials_of(b) * sizeof(float); }
+
+int defl_mx4_quantize(defl_ctx* c, const void* X, int dtype, int b, int rows, int cols, int64_t ld, int64_t batch_stride, int fmt,
+                      const defl_mx4* by_rows, const defl_mx4* by_cols, void* work) {
+  if (!c || !X || b <= 0 || rows <= 0 || cols <= 0 || ld < cols || (b > 1 && batch_stride < 0)) return DEFL_ERR_ARG;
+  if ((dtype != DEFL_BF16 && dtype != DEFL_F32) || (fmt != DEFL_MXFP4 && fmt != DEFL_NVFP4)) return DEFL_ERR_ARG;
+  if ((!by_rows && !by_cols) || (by_rows && !matrix_ok(by_rows, fmt)) || (by_cols && !matrix_ok(by_cols, fmt))) return DEFL_ERR_ARG;
+  const unsigned es = (unsigned)dtype_size(dtype);
+  if (!on(X, es)) return DEFL_ERR_ARG;
+  if (rows > DEFL_MX4_MAX_SIDE || cols > DEFL_MX4_MAX_SIDE || b > 65535) return DEFL_ERR_RANK;
+  const bool scan = (long long)rows * cols <= SCAN_MOST;
+  if (fmt == DEFL_NVFP4 && !scan && (!work || !on(work, 4))) return DEFL_ERR_ARG;
+  DeviceScope scope(c->device);
+  c->err[0] = 0;
+  QuantParams p = {};
+  p.X = X; p.ld = ld; p.batch_stride = batch_stride; p.b = b; p.rows = rows; p.cols = cols;
+  p.tiles_c = (cols + TILE - 1) / TILE;
+  if ((long long)p.tiles_c * ((rows + TILE - 1) / TILE) > 0x7fffffffll) return DEFL_ERR_RANK;
+  if (by_rows) { p.rc = (uint8_t*)by_rows->codes; p.rs = (uint8_t*)by_rows->scales; p.rscale = fmt == DEFL_NVFP4 ? by_rows->scale : nullptr; }
+  if (by_cols) { p.cc = (uint8_t*)by_cols->codes; p.cs = (uint8_t*)by_cols->scales; p.cscale = fmt == DEFL_NVFP4 ? by_cols->scale : nullptr; }
+  const bool vec = on(X, 16) && (ld * es) % 16 == 0 && (b == 1 || (batch_stride * es) % 16 == 0);
+  if (fmt == DEFL_NVFP4 && !scan) {
+    p.nper = partials_of(b);
+    p.partial = reinterpret_cast<const float*>(work);
+    const cudaError_t e = dtype == DEFL_BF16 ? amax_launch<__nv_bfloat16>(X, ld, batch_stride, rows, cols, b, p.nper, (float*)work, vec, c->stream)
+                                             : amax_launch<float>(X, ld, batch_stride, rows, cols, b, p.nper, (float*)work, vec, c->stream);
+    ++c->launches;
+    if (ctx_fail(c, e, "mx4 largest magnitude")) return DEFL_ERR_CUDA;
+  }
+  cudaError_t e;
+  if (dtype == DEFL_BF16) e = fmt == DEFL_MXFP4 ? quantize_launch<__nv_bfloat16, MXFP4>(p, vec, c->stream) : quantize_launch<__nv_bfloat16, NVFP4>(p, vec, c->stream);
+  else e = fmt == DEFL_MXFP4 ? quantize_launch<float, MXFP4>(p, vec, c->stream) : quantize_launch<float, NVFP4>(p, vec, c->stream);
+  ++c->launches;
+  if (ctx_fail(c, e, "mx4 quantize")) return DEFL_ERR_CUDA;
+  return DEFL_OK;
+}
+
+int defl_mx4_dequantize(defl_ctx* c, const defl_mx4* a, int b, int rows, int cols, int fmt, void* out, int dtype) {
+  if (!c || !a || !out || b <= 0 || rows <= 0 || cols <= 0) return DEFL_ERR_ARG;
+  if ((dtype != DEFL_BF16 && dtype != DEFL_F32) || (fmt != DEFL_MXFP4 && fmt != DEFL_NVFP4) || !matrix_ok(a, fmt)) return DEFL_ERR_ARG;
+  if (!on(out, (unsigned)dtype_size(dtype))) return DEFL_ERR_ARG;
+  if (rows > DEFL_MX4_MAX_SIDE || cols > DEFL_MX4_MAX_SIDE) return DEFL_ERR_RANK;
+  const long long grid = ((long long)b * rows + Q_THREADS / 32 - 1) / (Q_THREADS / 32);
+  if (grid > 0x7fffffffll) return DEFL_ERR_RANK;
+  DeviceScope scope(c->device);
+  c->err[0] = 0;
+  const Mx4View v = {(const uint8_t*)a->codes, (const uint8_t*)a->scales, a->scale};
+  const int vec = on(out, 16) && cols % 8 == 0;
+  const dim3 g((unsigned)grid), t(Q_THREADS);
+  cudaError_t e;
+  if (dtype == DEFL_BF16) {
+    __nv_bfloat16* o = (__nv_bfloat16*)out;
+    e = fmt == DEFL_MXFP4 ? launch_kernel(mx4_dequantize_kernel<MXFP4, __nv_bfloat16>, g, t, 0, c->stream, v, b, rows, cols, o, vec)
+                          : launch_kernel(mx4_dequantize_kernel<NVFP4, __nv_bfloat16>, g, t, 0, c->stream, v, b, rows, cols, o, vec);
+  } else {
+    float* o = (float*)out;
+    e = fmt == DEFL_MXFP4 ? launch_kernel(mx4_dequantize_kernel<MXFP4, float>, g, t, 0, c->stream, v, b, rows, cols, o, vec)
+                          : launch_kernel(mx4_dequantize_kernel<NVFP4, float>, g, t, 0, c->stream, v, b, rows, cols, o, vec);
+  }
+  ++c->launches;
+  if (ctx_fail(c, e, "mx4 dequantize")) return DEFL_ERR_CUDA;
+  return DEFL_OK;
+}
+
+int defl_mx4_gemm(defl_ctx* c, const defl_mx4* A, const defl_mx4* B, int b, int M, int N, int K, int b_shared, int fmt, float alpha, void* D, int64_t ldd,
+                  int64_t batch_stride, int out_dtype) {
+  if (!c || !A || !B || !D || b <= 0 || M <= 0 || N <= 0 || K <= 0 || ldd < N) return DEFL_ERR_ARG;
+  if (b > 1 && batch_stride < (int64_t)(M - 1) * ldd + N) return DEFL_ERR_ARG;
+  if ((fmt != DEFL_MXFP4 && fmt != DEFL_NVFP4) || (out_dtype != DEFL_BF16 && out_dtype != DEFL_F32)) return DEFL_ERR_ARG;
+  if (!matrix_ok(A, fmt) || !matrix_ok(B, fmt) || !on(D, (unsigned)dtype_size(out_dtype))) return DEFL_ERR_ARG;
+  if (M > DEFL_MX4_MAX_SIDE || N > DEFL_MX4_MAX_SIDE || K > DEFL_MX4_MAX_SIDE || b > 65535) return DEFL_ERR_RANK;
+  DeviceScope scope(c->device);
+  c->err[0] = 0;
+  Mx4Gemm g;
+  g.A = {(const uint8_t*)A->codes, (const uint8_t*)A->scales, A->scale};
+  g.B = {(const uint8_t*)B->codes, (const uint8_t*)B->scales, B->scale};
+  g.b = b; g.M = M; g.N = N; g.K = K; g.fmt = fmt; g.b_shared = b_shared != 0;
+  g.D = D; g.ldd = ldd; g.batch_d = batch_stride; g.out_dtype = out_dtype; g.alpha = alpha;
+  const unsigned long long wait_ns = (unsigned long long)(c->tc_knobs.wait_ms > 0 ? c->tc_knobs.wait_ms : 2000) * 1000000ull;
+  if (ctx_fail(c, mx4_gemm_launch(g, c->stream, c->wait_status, c->num_sms, wait_ns, &c->launches), "mx4 gemm")) return DEFL_ERR_CUDA;
+  return DEFL_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,28 @@
+// Microscaled 4-bit matrices as the kernels see them (layout and definitions: include/defl.h), and what both files share.
+#pragma once
+#include "common.cuh"
+
+namespace defl {
+
+enum Mx4Format { MXFP4 = 0, NVFP4 = 1 };
+
+__host__ __device__ inline int mx4_width(int cols) { return (cols + 31) & ~31; }                      // codes a row, padded
+__host__ __device__ inline int mx4_row_tiles(int rows) { return (rows + 127) >> 7; }
+__host__ __device__ inline int mx4_scale_tiles(int cols, int fmt) {                                   // tiles of four blocks
+  return fmt == MXFP4 ? (mx4_width(cols) + 127) >> 7 : (mx4_width(cols) + 63) >> 6;
+}
+
+struct Mx4View { const uint8_t* codes; const uint8_t* scales; const float* scale; };
+
+// D [b, M, N] = alpha * A B^T; b_shared: the same B for all
+struct Mx4Gemm {
+  Mx4View A, B;
+  int b, M, N, K, fmt, b_shared;
+  void* D; long long ldd, batch_d; int out_dtype;
+  float alpha;
+};
+cudaError_t mx4_gemm_prepare();
+cudaError_t mx4_quantize_prepare();
+cudaError_t mx4_gemm_launch(const Mx4Gemm& g, cudaStream_t st, int* status, int num_sms, unsigned long long wait_ns, long long* launches);
+
+}  // namespace defl

@@ -1,0 +1,605 @@
+// Products of microscaled 4-bit matrices for sm_100a: D = alpha A B^T.
+//
+// mx4_tc_kernel, the tensor cores' form: persistent and warp-specialised like the 16-bit engine (gemm_tc.cu): warp 0 copies
+// operand tiles and their scales into a ring of shared-memory stages, warp 1 issues the products, warps 2..9 read the accumulators
+// out. A stage covers 256 values of K (128 bytes a row, 128-byte swizzle). The scales travel as they lie in memory, in tiles of 128 rows
+// x 4 blocks (512 bytes), and go from shared to tensor memory with tcgen05.cp, which replicates them over the four lane
+// quarters; a product takes 64 values of K and reads its scales there.
+//   M > 128   a pair of CTAs per 256 x BN tile (cta_group::2): each stages 128 rows of A, half of the B columns, the scales of its own
+//             rows and those of all columns (each multiplies its rows with all of them)
+//   M <= 128  one CTA, 128 x BN
+// Tensor memory: 512 columns = two accumulators and 64 columns of scales. Two accumulators of 256 columns leave no room, so they
+// overlap by 64 columns; the read-out takes those first and says so, and the next tile's products wait for that much only.
+// What bounds it: at 4.5 PFLOP/s and more the operands of a 256 x 256 tile (64 + 6 KB per 256 values of K and pair) come at what
+// L2 delivers to the whole chip, 5500 bytes a cycle; short K is bound by the read-out and by writing D.
+//
+// mx4_row_kernel, for up to eight rows of A: the weights are read once at memory speed, each code becomes two bytes by table
+// lookup (prmt), four products at a time are integer dot products (dp4a), a block's sum meets its scales in fp32.
+#include "ctx.cuh"
+#include "mx4.cuh"
+#include "tc_ptx.cuh"
+#include <cuda_fp8.h>
+#include <cudaTypedefs.h>
+#include <mutex>
+
+namespace defl {
+
+namespace {
+
+constexpr int KB_ELEMENTS = 256, KB_BYTES = 128;
+constexpr int TC_THREADS = 320, TC_EPI_WARPS = 8;
+constexpr int MAX_ST = 8;
+constexpr int STG_BYTES = 4096;                    // 32 rows x 128 bytes
+constexpr uint32_t SF_COL = 448;                   // tensor-memory columns of the scales: A's, then (16 further) B's
+constexpr uint32_t SMEM_MOST = 227 * 1024;
+
+struct TcParams4 {
+  CUtensorMap tmA, tmB, tmSA, tmSB, tmD;
+  int M, N, batch, BN, b_shared;
+  int tiles_m, tiles_n;
+  int total_tiles;
+  int kblocks, ksteps_last;                        // stages a tile, and products of 64 values in the last of them
+  int stages, nsb, overlap, stg_bufs;
+  uint32_t a_bytes, b_bytes, sf_bytes, stage_bytes;
+  uint32_t idesc;
+  int out_f32, store_tma;
+  void* D; long long ldd, batch_d;
+  float alpha; const float* scale_a; const float* scale_b;
+  int* status; unsigned long long wait_ns;
+};
+
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, "
+      "%28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+        "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+
+// 512 bytes of scales (32 rows of 16 bytes, no swizzle: groups of eight rows 128 bytes apart) to four columns of all lane quarters
+template <int PAIR>
+__device__ __forceinline__ void scales_to_tmem(uint32_t tcol, uint32_t saddr) {
+  const uint64_t desc = (uint64_t)((saddr >> 4) & 0x3FFFu) | (uint64_t)1 << 16 | (uint64_t)(128u >> 4) << 32 | (uint64_t)1 << 46;
+  if (PAIR) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tcol), "l"(desc) : "memory");
+  else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tcol), "l"(desc) : "memory");
+}
+
+template <int FMT, int PAIR>
+__device__ __forceinline__ void umma4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
+#define DEFL_MX4_MMA(GROUP, KIND)                                                                                    \
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"                                                     \
+               "tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], %1, %2, %3, [%4], [%5], p;\n\t}"               \
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory")
+  if (FMT == MXFP4) {
+    if (PAIR) DEFL_MX4_MMA("2", "mxf4.block_scale.scale_vec::2X"); else DEFL_MX4_MMA("1", "mxf4.block_scale.scale_vec::2X");
+  } else {
+    if (PAIR) DEFL_MX4_MMA("2", "mxf4nvf4.block_scale.scale_vec::4X"); else DEFL_MX4_MMA("1", "mxf4nvf4.block_scale.scale_vec::4X");
+  }
+#undef DEFL_MX4_MMA
+}
+
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* tm, uint32_t src, int c0, int c1, int c2) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
+               ::"l"(tm), "r"(src), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+
+struct Tile4 { int bz, tm, tn, n_eff; };
+template <int PAIR>
+__device__ __forceinline__ Tile4 tile_of(const TcParams4& p, int tile) {
+  Tile4 t;
+  const int per = p.tiles_m * p.tiles_n;
+  t.bz = tile / per;
+  const int i = tile - t.bz * per;
+  t.tn = i / p.tiles_m;                            // tiles of one column of tiles follow one another: they share B
+  t.tm = i - t.tn * p.tiles_m;
+  const int left = p.N - t.tn * p.BN, q = PAIR ? 31 : 15;
+  t.n_eff = min(p.BN, (left + q) & ~q);
+  return t;
+}
+
+template <int FMT, int PAIR>
+__global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_constant__ TcParams4 p) {
+  constexpr int ATOMS = FMT == MXFP4 ? 2 : 4;      // tiles of scales a row tile and stage
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t full_bar[MAX_ST], empty_bar[MAX_ST], acc_full_bar[2], acc_empty_bar[2], ovl_bar;
+  __shared__ uint32_t tmem_base_slot;
+  __shared__ int abort_flag;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
+  const int tile0 = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x, tile_step = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x;
+  constexpr int TILE_M = PAIR ? 256 : 128;
+
+  if (warp == 2 && lane == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&p.tmA) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&p.tmB) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&p.tmSA) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&p.tmSB) : "memory");
+  }
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    for (int s = 0; s < p.stages; ++s) { mbar_init(smem_u32(&full_bar[s]), 1); mbar_init(smem_u32(&empty_bar[s]), 1); }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(smem_u32(&acc_full_bar[a]), 1);
+      mbar_init(smem_u32(&acc_empty_bar[a]), (PAIR ? 2 : 1) * TC_EPI_WARPS);
+    }
+    mbar_init(smem_u32(&ovl_bar), (PAIR ? 2 : 1) * TC_EPI_WARPS);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    if (PAIR) { tmem_alloc_pair(smem_u32(&tmem_base_slot), 512); tmem_relinquish_pair(); }
+    else { tmem_alloc(smem_u32(&tmem_base_slot), 512); tmem_relinquish(); }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (PAIR) cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_base_slot;
+  pdl_launch();
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------ copies: every lane of the step's issues one
+    const uint32_t full0 = smem_u32(&full_bar[0]), empty0 = smem_u32(&empty_bar[0]);
+    const uint32_t full0_sig = PAIR ? map_to_cta(full0, 0) : full0;
+    const uint32_t tx = (PAIR ? 2u : 1u) * p.stage_bytes;
+    constexpr int XS = ATOMS / 2;                  // boxes of 1024 bytes of scales a row tile and stage
+    // lane 0: A, 1: B, then A's scales, then B's
+    const int idx = lane - 2;
+    const bool is_sa = idx >= 0 && idx < XS, is_sb = idx >= XS && idx < XS * (1 + p.nsb);
+    const int sb_rt = is_sb ? (idx - XS) / XS : 0, part = is_sa ? idx : is_sb ? (idx - XS) % XS : 0;
+    const bool on = lane < 2 || is_sa || is_sb;
+    const CUtensorMap* tm = lane == 0 ? &p.tmA : lane == 1 ? &p.tmB : is_sa ? &p.tmSA : &p.tmSB;
+    const uint32_t off = lane == 0 ? 0u : lane == 1 ? p.a_bytes
+                         : p.a_bytes + p.b_bytes + (is_sa ? 0u : (uint32_t)(1 + sb_rt) * p.sf_bytes) + (uint32_t)part * 1024u;
+    uint32_t stage = 0, phase = 0;
+    bool live = true;
+    pdl_wait();
+    for (int tile = tile0; tile < p.total_tiles && live; tile += tile_step) {
+      const Tile4 t = tile_of<PAIR>(p, tile);
+      const int n0 = t.tn * p.BN, m0 = t.tm * TILE_M + (int)rank * 128;
+      const int bz_b = p.b_shared ? 0 : t.bz;
+      const int c1 = lane == 0 ? m0 : lane == 1 ? n0 + (PAIR ? (int)rank * (t.n_eff >> 1) : 0) : is_sa ? m0 >> 7 : (n0 >> 7) + sb_rt;
+      const int c2 = (lane == 0 || is_sa) ? t.bz : bz_b;
+      for (int kb = 0; kb < p.kblocks; ++kb) {
+        int ok = 1;
+        if (lane == 0) ok = mbar_wait(empty0 + 8u * stage, phase ^ 1u, &abort_flag, p.status, p.wait_ns) ? 1 : 0;
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        if (!ok) { live = false; break; }
+        if (lane == 0 && rank == 0) mbar_expect_tx(full0 + 8u * stage, tx);
+        if (on) {
+          const uint32_t dst = smem_base + stage * p.stage_bytes + off, bar = full0_sig + 8u * stage;
+          const int c0 = lane < 2 ? kb * KB_BYTES : kb * (ATOMS * 128) + part * 256;
+          if (PAIR) tma_load_3d_pair(dst, tm, bar, c0, c1, c2); else tma_load_3d(dst, tm, bar, c0, c1, c2);
+        }
+        __syncwarp();
+        if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ products
+    if (lane == 0 && rank == 0) {
+      const uint64_t hi = smem_desc_hi(16u, 1024u);
+      const uint32_t full0 = smem_u32(&full_bar[0]), empty0 = smem_u32(&empty_bar[0]);
+      const uint32_t acc1 = p.overlap ? SF_COL - 256u : 256u;
+      const uint32_t sa_col = tmem_base + SF_COL, sb_col = tmem_base + SF_COL + 16u;
+      uint32_t stage = 0, phase = 0;
+      pdl_wait();
+      for (int tile = tile0, it = 0; tile < p.total_tiles; tile += tile_step, ++it) {
+        const Tile4 t = tile_of<PAIR>(p, tile);
+        const uint32_t acc = (uint32_t)it & 1u, use = ((uint32_t)it >> 1) & 1u;
+        if (!mbar_wait(smem_u32(&acc_empty_bar[acc]), use ^ 1u, &abort_flag, p.status, p.wait_ns)) break;
+        if (p.overlap && it > 0 && !mbar_wait(smem_u32(&ovl_bar), (uint32_t)(it - 1) & 1u, &abort_flag, p.status, p.wait_ns)) break;
+        tc_fence_after();
+        const uint32_t d = tmem_base + (acc ? acc1 : 0u);
+        const uint32_t idesc = p.idesc | ((uint32_t)(t.n_eff >> 3) << 17);
+        const uint32_t shift = (uint32_t)((t.tn * p.BN) & 127) >> 5;      // B's first row within its tile of scales, in columns
+        bool ok = true;
+        for (int kb = 0; kb < p.kblocks; ++kb) {
+          if (!mbar_wait(full0 + 8u * stage, phase, &abort_flag, p.status, p.wait_ns)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t sA = smem_base + stage * p.stage_bytes, sB = sA + p.a_bytes, sS = sB + p.b_bytes;
+          const int ksteps = kb + 1 < p.kblocks ? 4 : p.ksteps_last;
+#pragma unroll
+          for (int a = 0; a < ATOMS; ++a) {
+            if (a * (4 / ATOMS) >= ksteps) break;
+            scales_to_tmem<PAIR>(sa_col + 4u * a, sS + 512u * a);
+            for (int r = 0; r < p.nsb; ++r) scales_to_tmem<PAIR>(sb_col + 4u * (uint32_t)(a * p.nsb + r), sS + (uint32_t)(1 + r) * p.sf_bytes + 512u * a);
+          }
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) {
+            if (kk >= ksteps) break;
+            const int a = FMT == MXFP4 ? kk >> 1 : kk;
+            const uint32_t id = FMT == MXFP4 ? (uint32_t)(kk & 1) * 2u : 0u;
+            umma4<FMT, PAIR>(d, hi | (uint64_t)((sA >> 4) + 2u * kk), hi | (uint64_t)((sB >> 4) + 2u * kk), idesc | id << 4 | id << 29,
+                             sa_col + 4u * a, sb_col + 4u * (uint32_t)(a * p.nsb) + shift, (kb | kk) ? 1u : 0u);
+          }
+          if (PAIR) umma_commit_pair(empty0 + 8u * stage); else umma_commit(empty0 + 8u * stage);
+          if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
+        }
+        if (!ok) break;
+        if (PAIR) umma_commit_pair(smem_u32(&acc_full_bar[acc])); else umma_commit(smem_u32(&acc_full_bar[acc]));
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------ read-out: 32 rows and every other chunk of columns a warp
+    const int q = warp & 3, wsel = (warp - 2) >> 2;
+    const uint32_t stg0 = smem_base + (uint32_t)p.stages * p.stage_bytes + (uint32_t)((warp - 2) * p.stg_bufs) * STG_BYTES;
+    const uint32_t acc1 = p.overlap ? SF_COL - 256u : 256u;
+    const uint32_t ovl_sig = PAIR ? map_to_cta(smem_u32(&ovl_bar), 0) : smem_u32(&ovl_bar);
+    const int cw = p.out_f32 ? 32 : 64;            // columns of 128 bytes
+    int buf = 0;
+    pdl_wait();
+    for (int tile = tile0, it = 0; tile < p.total_tiles; tile += tile_step, ++it) {
+      const Tile4 t = tile_of<PAIR>(p, tile);
+      const uint32_t acc = (uint32_t)it & 1u, use = ((uint32_t)it >> 1) & 1u;
+      float alpha = p.alpha;
+      if (FMT == NVFP4) alpha *= p.scale_a[t.bz] * p.scale_b[p.b_shared ? 0 : t.bz];
+      if (!mbar_wait(smem_u32(&acc_full_bar[acc]), use, &abort_flag, p.status, p.wait_ns)) break;
+      tc_fence_after();
+      const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (acc ? acc1 : 0u);
+      const int row0 = t.tm * TILE_M + (int)rank * 128 + q * 32, n0 = t.tn * p.BN;
+      const int chunks = (t.n_eff + cw - 1) / cw, ovl_chunks = 64 / cw, full = p.BN / cw;
+      bool told = !p.overlap;
+      // the overlapping columns come first: the last ones of the first accumulator, the first ones of the second
+      for (int i = wsel; i < full; i += 2) {
+        if (!told && i >= ovl_chunks) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) { if (PAIR) mbar_arrive_cluster(ovl_sig); else mbar_arrive(ovl_sig); }
+          told = true;
+        }
+        const int c = (p.overlap && acc == 0) ? full - 1 - i : i;
+        if (c >= chunks || row0 >= p.M) continue;
+        const int col0 = c * cw;
+        uint32_t r[64];
+        tmem_ld32(taddr + col0, r);
+        if (!p.out_f32) tmem_ld32(taddr + col0 + 32, r + 32);
+        const uint32_t stg = stg0 + (uint32_t)buf * STG_BYTES;
+        // the buffer's last store has read it
+        if (p.stg_bufs == 2) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        __syncwarp();
+        tmem_ld_wait();
+#pragma unroll
+        for (int pc = 0; pc < 8; ++pc) {
+          uint32_t w[4];
+          if (p.out_f32) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = __float_as_uint(alpha * __uint_as_float(r[4 * pc + j]));
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = pack16x2(alpha * __uint_as_float(r[8 * pc + 2 * j]), alpha * __uint_as_float(r[8 * pc + 2 * j + 1]), false);
+          }
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stg + (uint32_t)lane * 128u + ((uint32_t)(pc ^ (lane & 7)) << 4)), "r"(w[0]),
+                       "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+        }
+        if (p.store_tma) {
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) {
+            if (n0 + col0 < p.N) tma_store_3d(&p.tmD, stg, n0 + col0, row0, t.bz);
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          }
+        } else {
+          // rows that the copy engine cannot address: 4 bytes of a row a lane, single elements
+          __syncwarp();
+          for (int rr = 0; rr < 32 && row0 + rr < p.M; ++rr) {
+            uint32_t w;
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(stg + (uint32_t)rr * 128u + ((uint32_t)((lane >> 2) ^ (rr & 7)) << 4) + 4u * (lane & 3)));
+            const long long at = (long long)t.bz * p.batch_d + (long long)(row0 + rr) * p.ldd + n0 + col0;
+            if (p.out_f32) {
+              if (n0 + col0 + lane < p.N) reinterpret_cast<uint32_t*>(p.D)[at + lane] = w;
+            } else {
+              if (n0 + col0 + 2 * lane < p.N) reinterpret_cast<uint16_t*>(p.D)[at + 2 * lane] = (uint16_t)w;
+              if (n0 + col0 + 2 * lane + 1 < p.N) reinterpret_cast<uint16_t*>(p.D)[at + 2 * lane + 1] = (uint16_t)(w >> 16);
+            }
+          }
+          __syncwarp();
+        }
+        if (p.stg_bufs == 2) buf ^= 1;
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (!told) { if (PAIR) mbar_arrive_cluster(ovl_sig); else mbar_arrive(ovl_sig); }
+        if (PAIR) mbar_arrive_cluster(map_to_cta(smem_u32(&acc_empty_bar[acc]), 0)); else mbar_arrive(smem_u32(&acc_empty_bar[acc]));
+      }
+      __syncwarp();
+    }
+    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");       // what is on its way to memory gets there before the CTA ends
+  }
+
+  // ------------------------------------------------------------------ teardown
+  tc_fence_before();
+  __syncthreads();
+  if (abort_flag && threadIdx.x == 0) {
+    // a wait ran out: copies that may still be in flight get a bounded time to land before the shared memory is released
+    const unsigned long long t0 = global_ns();
+    while (global_ns() - t0 < 2000000ull) { }
+  }
+  __syncthreads();
+  if (PAIR) cluster_sync_all();
+  if (warp == 1) {
+    tc_fence_after();
+    if (PAIR) tmem_dealloc_pair(tmem_base, 512); else tmem_dealloc(tmem_base, 512);
+  }
+}
+
+// ----------------------------------------------------------------------------- up to eight rows
+constexpr int ROW_THREADS = 256, ROW_CHUNK = 4096;     // values of K that are staged at a time
+
+__device__ __forceinline__ uint32_t lookup(uint32_t sel) {
+  // twice the magnitudes 0 .5 1 1.5 2 3 4 6, one byte for each of four codes; codes with the sign bit give zero (prmt's sign mode)
+  uint32_t r;
+  asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(0x03020100u), "r"(0x0C080604u), "r"(sel));
+  return r;
+}
+template <int FMT>
+__device__ __forceinline__ float scale_value(uint32_t byte) {
+  if (FMT == MXFP4) return byte == 255u ? __uint_as_float(0x7fffffffu) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
+  return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)byte, __NV_E4M3)));
+}
+
+struct RowParams {
+  Mx4View A, B;
+  int M, N, K, b_shared;
+  void* D; long long ldd, batch_d; int out_f32;
+  float alpha;
+};
+
+// LPR lanes a row of B: 16 where there are rows enough, else the whole CTA. T >= M rows of A.
+template <int FMT, int T, int LPR>
+__global__ void __launch_bounds__(ROW_THREADS) mx4_row_kernel(const RowParams p) {
+  constexpr int BLK = FMT == MXFP4 ? 32 : 16, NB = 32 / BLK;
+  __shared__ __align__(16) int8_t s_a[T][ROW_CHUNK];
+  __shared__ float s_sc[T][ROW_CHUNK / BLK];
+  __shared__ float s_part[ROW_THREADS / 32][T];
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int bz = blockIdx.y;
+  const int width = mx4_width(p.K), pieces = width / 32, kt = mx4_scale_tiles(p.K, FMT);
+  const long long n = (long long)blockIdx.x * (ROW_THREADS / LPR) + tid / LPR;
+  const bool row_ok = n < p.N;
+  const int at0 = tid % LPR;
+  const int bb = p.b_shared ? 0 : bz;
+  const uint4* const w = reinterpret_cast<const uint4*>(p.B.codes + ((long long)bb * p.N + (row_ok ? n : 0)) * (width / 2));
+  const int nr = row_ok ? (int)n : 0;
+  const uint8_t* const ws = p.B.scales + ((long long)bb * mx4_row_tiles(p.N) + (nr >> 7)) * kt * 512 + (nr & 31) * 16 + ((nr >> 5) & 3) * 4;
+  const uint8_t* const ac = p.A.codes + (long long)bz * p.M * (width / 2);
+  const uint8_t* const as = p.A.scales + (long long)bz * mx4_row_tiles(p.M) * kt * 512;
+  float sum[T];
+#pragma unroll
+  for (int t = 0; t < T; ++t) sum[t] = 0.f;
+  pdl_wait();
+  for (int k0 = 0; k0 < width; k0 += ROW_CHUNK) {
+    const int kn = min(ROW_CHUNK, width - k0);
+    if (k0) __syncthreads();
+    for (int u = tid; u < T * (kn / 8); u += ROW_THREADS) {
+      const int t = u / (kn / 8), o = u - t * (kn / 8);
+      uint32_t codes = 0;
+      if (t < p.M) codes = *reinterpret_cast<const uint32_t*>(ac + (long long)t * (width / 2) + k0 / 2 + 4 * o);
+      // signed bytes: the positive ones less the negative ones, byte by byte
+      const uint32_t lo = __vsub4(lookup(codes & 0xffffu), lookup((codes & 0xffffu) ^ 0x8888u));
+      const uint32_t hi = __vsub4(lookup(codes >> 16), lookup((codes >> 16) ^ 0x8888u));
+      *reinterpret_cast<uint2*>(&s_a[t][8 * o]) = make_uint2(lo, hi);
+    }
+    for (int u = tid; u < T * (kn / BLK); u += ROW_THREADS) {
+      const int t = u / (kn / BLK), j = u - t * (kn / BLK), blk = k0 / BLK + j;
+      float s = 0.f;
+      if (t < p.M) s = 0.25f * scale_value<FMT>(as[(long long)(blk >> 2) * 512 + (t & 31) * 16 + (blk & 3)]);
+      s_sc[t][j] = s;
+    }
+    __syncthreads();
+    if (row_ok) {
+      const int first = k0 / 32, last = min(pieces, first + ROW_CHUNK / 32);
+#pragma unroll 4
+      for (int i = first + at0; i < last; i += LPR) {
+        const uint4 q = w[i];
+        uint32_t sb;
+        if (FMT == MXFP4) sb = ws[(long long)(i >> 2) * 512 + (i & 3)];
+        else sb = *reinterpret_cast<const uint16_t*>(ws + (long long)(i >> 1) * 512 + (i & 1) * 2);
+        const uint32_t c[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+          const uint4* a4 = reinterpret_cast<const uint4*>(&s_a[t][(i - first) * 32]);
+          const uint4 a0 = a4[0], a1 = a4[1];
+          const uint32_t a[8] = {a0.x, a0.y, a0.z, a0.w, a1.x, a1.y, a1.z, a1.w};
+#pragma unroll
+          for (int h = 0; h < NB; ++h) {
+            int pos = 0, neg = 0;
+#pragma unroll
+            for (int j = 0; j < 4 / NB; ++j) {
+              const uint32_t x = c[h * (4 / NB) + j];
+              const int al = (int)a[2 * (h * (4 / NB) + j)], ah = (int)a[2 * (h * (4 / NB) + j) + 1];
+              pos = __dp4a((int)lookup(x & 0xffffu), al, pos);
+              neg = __dp4a((int)lookup((x & 0xffffu) ^ 0x8888u), al, neg);
+              pos = __dp4a((int)lookup(x >> 16), ah, pos);
+              neg = __dp4a((int)lookup((x >> 16) ^ 0x8888u), ah, neg);
+            }
+            // (the sum meets one scale after the other: their product alone may leave fp32's range)
+            sum[t] += (float)(pos - neg) * s_sc[t][(i - first) * NB + h] * scale_value<FMT>(h ? sb >> 8 : sb & 0xffu);
+          }
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int o = (LPR < 32 ? LPR : 32) / 2; o > 0; o >>= 1) sum[t] += __shfl_xor_sync(0xffffffffu, sum[t], o);
+  if (LPR > 32) {
+    if (lane == 0)
+#pragma unroll
+      for (int t = 0; t < T; ++t) s_part[tid >> 5][t] = sum[t];
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      sum[t] = 0.f;
+      for (int k = 0; k < ROW_THREADS / 32; ++k) sum[t] += s_part[k][t];
+    }
+  }
+  if (row_ok && at0 == 0) {
+    float alpha = p.alpha;
+    if (FMT == NVFP4) alpha *= p.A.scale[bz] * p.B.scale[bb];
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+      if (t < p.M) {
+        const long long at = (long long)bz * p.batch_d + (long long)t * p.ldd + n;
+        if (p.out_f32) reinterpret_cast<float*>(p.D)[at] = alpha * sum[t];
+        else reinterpret_cast<__nv_bfloat16*>(p.D)[at] = __float2bfloat16_rn(alpha * sum[t]);
+      }
+  }
+}
+
+// ----------------------------------------------------------------------------- host side
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn encode_fn() {
+  static EncodeFn fn = nullptr;
+  static std::once_flag once;
+  std::call_once(once, [] {
+    void* ptr = nullptr;
+    cudaDriverEntryPointQueryResult r;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &r) == cudaSuccess && r == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<EncodeFn>(ptr);
+  });
+  return fn;
+}
+
+// [batch, rows, inner] of elements of `es` bytes, boxes of box_inner x box_rows
+bool encode(CUtensorMap* tm, CUtensorMapDataType type, const void* base, long long inner, long long rows, long long batch, long long row_bytes,
+            long long batch_bytes, uint32_t box_inner, uint32_t box_rows, bool swizzle) {
+  const cuuint64_t dims[3] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)batch};
+  const cuuint64_t strides[2] = {(cuuint64_t)row_bytes, (cuuint64_t)batch_bytes};
+  const cuuint32_t box[3] = {box_inner, box_rows, 1}, est[3] = {1, 1, 1};
+  return encode_fn()(tm, type, 3, const_cast<void*>(base), dims, strides, box, est, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                     swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Tile width: the one with the smallest modelled time in cycles. A stage takes the tensor pipe 2 cycles a column, at least what a step
+// of the issuing thread takes, at least its operand bytes at the 5500 bytes a cycle that L2 delivers to the chip; the read-out of a
+// tile overlaps the next tile's stages, except the last.
+int choose_width(const Mx4Gemm& g, bool pair, int num_sms) {
+  static const int widths[4] = {256, 192, 128, 64};      // (64 bf16 columns are the read-out's 128 bytes)
+  const int slots = pair ? num_sms / 2 : num_sms, tm = (g.M + (pair ? 255 : 127)) / (pair ? 256 : 128);
+  const double kb = (g.K + KB_ELEMENTS - 1) / KB_ELEMENTS;
+  int best = 0;
+  double best_t = 0.0;
+  for (int bn : widths) {
+    if (bn > 64 && bn / 2 >= g.N) continue;
+    const double tiles = (double)g.b * tm * ((g.N + bn - 1) / bn), waves = (double)(long long)((tiles + slots - 1) / slots);
+    const double live = (tiles < slots ? tiles : slots) * (pair ? 2 : 1);
+    double step = 2.0 * bn;
+    if (step < 300.0) step = 300.0;
+    const double bytes = (128.0 + (pair ? bn / 2 : bn)) * KB_BYTES + 3072.0;
+    if (step < bytes * live / 5500.0) step = bytes * live / 5500.0;
+    const double out = 1000.0 + bn * (g.out_dtype == F32 ? 16.0 : 10.0);
+    const double t = (waves - 1.0) * (kb * step > out ? kb * step : out) + kb * step + out;
+    if (!best || t < best_t) { best = bn; best_t = t; }
+  }
+  return best;
+}
+
+template <int FMT, int PAIR>
+cudaError_t tc_start(const TcParams4& p, int grid, size_t smem, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(TC_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cfg.attrs = attr; cfg.numAttrs = PAIR ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, mx4_tc_kernel<FMT, PAIR>, p);
+}
+
+template <int FMT, int T>
+cudaError_t row_start(const RowParams& p, int b, int num_sms, cudaStream_t st) {
+  // rows enough for two CTAs of sixteen rows on every SM, or long ones would leave most of the chip idle
+  if (p.N >= num_sms * 4) return launch_kernel(mx4_row_kernel<FMT, T, 16>, dim3((unsigned)((p.N + 15) / 16), (unsigned)b), dim3(ROW_THREADS), 0, st, p);
+  return launch_kernel(mx4_row_kernel<FMT, T, ROW_THREADS>, dim3((unsigned)p.N, (unsigned)b), dim3(ROW_THREADS), 0, st, p);
+}
+template <int FMT>
+cudaError_t row_pick(const RowParams& p, int b, int num_sms, cudaStream_t st) {
+  if (p.M == 1) return row_start<FMT, 1>(p, b, num_sms, st);
+  if (p.M == 2) return row_start<FMT, 2>(p, b, num_sms, st);
+  if (p.M <= 4) return row_start<FMT, 4>(p, b, num_sms, st);
+  return row_start<FMT, 8>(p, b, num_sms, st);
+}
+
+}  // namespace
+
+cudaError_t mx4_gemm_prepare() {
+  cudaError_t e;
+  if ((e = cudaFuncSetAttribute(mx4_tc_kernel<MXFP4, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST - 1024)) != cudaSuccess) return e;
+  if ((e = cudaFuncSetAttribute(mx4_tc_kernel<MXFP4, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST - 1024)) != cudaSuccess) return e;
+  if ((e = cudaFuncSetAttribute(mx4_tc_kernel<NVFP4, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST - 1024)) != cudaSuccess) return e;
+  return cudaFuncSetAttribute(mx4_tc_kernel<NVFP4, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST - 1024);
+}
+
+cudaError_t mx4_gemm_launch(const Mx4Gemm& g, cudaStream_t st, int* status, int num_sms, unsigned long long wait_ns, long long* launches) {
+  if (g.M <= 8) {
+    RowParams r;
+    r.A = g.A; r.B = g.B; r.M = g.M; r.N = g.N; r.K = g.K; r.b_shared = g.b_shared;
+    r.D = g.D; r.ldd = g.ldd; r.batch_d = g.batch_d; r.out_f32 = g.out_dtype == F32; r.alpha = g.alpha;
+    if (launches) ++*launches;
+    return g.fmt == MXFP4 ? row_pick<MXFP4>(r, g.b, num_sms, st) : row_pick<NVFP4>(r, g.b, num_sms, st);
+  }
+  if (!encode_fn()) return cudaErrorNotSupported;
+  const bool pair = g.M > 128;
+  TcParams4 p;
+  p.M = g.M; p.N = g.N; p.batch = g.b; p.b_shared = g.b_shared;
+  p.BN = choose_width(g, pair, num_sms);
+  p.tiles_m = (g.M + (pair ? 255 : 127)) / (pair ? 256 : 128);
+  p.tiles_n = (g.N + p.BN - 1) / p.BN;
+  const long long total = (long long)p.tiles_m * p.tiles_n * g.b;
+  if (total > 0x3fffffff) return cudaErrorInvalidValue;
+  p.total_tiles = (int)total;
+  const int width = mx4_width(g.K), kt = mx4_scale_tiles(g.K, g.fmt), atoms = g.fmt == MXFP4 ? 2 : 4;
+  p.kblocks = (width + KB_ELEMENTS - 1) / KB_ELEMENTS;
+  p.ksteps_last = (width - (p.kblocks - 1) * KB_ELEMENTS + 63) / 64;
+  p.nsb = p.BN <= 128 ? 1 : 2;
+  p.overlap = p.BN == 256;
+  const uint32_t b_rows = (uint32_t)(pair ? p.BN / 2 : p.BN);
+  p.a_bytes = 128 * KB_BYTES; p.b_bytes = b_rows * KB_BYTES; p.sf_bytes = (uint32_t)atoms * 512u;
+  p.stage_bytes = p.a_bytes + p.b_bytes + (uint32_t)(1 + p.nsb) * p.sf_bytes;
+  p.stg_bufs = 2;
+  const uint32_t stg = (uint32_t)(TC_EPI_WARPS * p.stg_bufs) * STG_BYTES, room = SMEM_MOST - 1024 - 1024 - stg;
+  p.stages = (int)(room / p.stage_bytes);
+  if (p.stages > MAX_ST) p.stages = MAX_ST;
+  const size_t smem = 1024 + (size_t)p.stages * p.stage_bytes + stg;
+  // kind::mxf4 / mxf4nvf4: e2m1 operands (1), both K-major; scales e8m0 (1) or e4m3 (0); M / 16 and N / 8 (added per tile)
+  p.idesc = 1u << 7 | 1u << 10 | (g.fmt == MXFP4 ? 1u : 0u) << 23 | (pair ? 16u : 8u) << 24;
+  p.out_f32 = g.out_dtype == F32;
+  p.D = g.D; p.ldd = g.ldd; p.batch_d = g.batch_d;
+  p.alpha = g.alpha; p.scale_a = g.A.scale; p.scale_b = g.B.scale;
+  p.status = status; p.wait_ns = wait_ns;
+  const long long es = p.out_f32 ? 4 : 2;
+  // (whole rows of 16-byte pieces: the copy engine writes the last piece in full, past a row that ends inside it)
+  p.store_tma = (reinterpret_cast<uintptr_t>(g.D) & 15u) == 0 && (g.N * es) % 16 == 0 && (g.ldd * es) % 16 == 0 && (g.b == 1 || (g.batch_d * es) % 16 == 0);
+  const int bb = g.b_shared ? 1 : g.b;
+  const long long rta = mx4_row_tiles(g.M), rtb = mx4_row_tiles(g.N);
+  bool ok = encode(&p.tmA, CU_TENSOR_MAP_DATA_TYPE_UINT8, g.A.codes, width / 2, g.M, g.b, width / 2, (long long)g.M * (width / 2), KB_BYTES, 128, true) &&
+            encode(&p.tmB, CU_TENSOR_MAP_DATA_TYPE_UINT8, g.B.codes, width / 2, g.N, bb, width / 2, (long long)g.N * (width / 2), KB_BYTES, b_rows, true) &&
+            encode(&p.tmSA, CU_TENSOR_MAP_DATA_TYPE_UINT32, g.A.scales, kt * 128ll, rta, g.b, kt * 512ll, rta * kt * 512ll, 256, 1, false) &&
+            encode(&p.tmSB, CU_TENSOR_MAP_DATA_TYPE_UINT32, g.B.scales, kt * 128ll, rtb, bb, kt * 512ll, rtb * kt * 512ll, 256, 1, false);
+  if (ok && p.store_tma) {
+    const long long batch_bytes = g.b > 1 ? g.batch_d * es : g.ldd * es * g.M;
+    ok = encode(&p.tmD, p.out_f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, g.D, g.N, g.M, g.b, g.ldd * es, batch_bytes,
+                p.out_f32 ? 32 : 64, 32, true);
+  }
+  if (!ok) return cudaErrorInvalidValue;
+  const int slots = pair ? num_sms / 2 : num_sms, runs = p.total_tiles < slots ? p.total_tiles : slots, grid = pair ? 2 * runs : runs;
+  if (launches) ++*launches;
+  if (g.fmt == MXFP4) return pair ? tc_start<MXFP4, 1>(p, grid, smem, st) : tc_start<MXFP4, 0>(p, grid, smem, st);
+  return pair ? tc_start<NVFP4, 1>(p, grid, smem, st) : tc_start<NVFP4, 0>(p, grid, smem, st);
+}
+
+}  // namespace defl

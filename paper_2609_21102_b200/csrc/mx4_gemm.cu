@@ -1,17 +1,18 @@
 // Products of microscaled 4-bit matrices for sm_100a: D = alpha A B^T.
 //
 // mx4_tc_kernel, the tensor cores' form: persistent and warp-specialised like the 16-bit engine (gemm_tc.cu): warp 0 copies
-// operand tiles and their scales into a ring of shared-memory stages, warp 1 issues the products, warps 2..9 read the accumulators
-// out. A stage covers 256 values of K (128 bytes a row, 128-byte swizzle). The scales travel as they lie in memory, in tiles of 128 rows
-// x 4 blocks (512 bytes), and go from shared to tensor memory with tcgen05.cp, which replicates them over the four lane
-// quarters; a product takes 64 values of K and reads its scales there.
+// operand tiles and their scales into a ring of shared-memory stages, warps 10..13 move the scales on to tensor memory, warp 1
+// issues the products, warps 2..9 read the accumulators out. A stage covers 256 values of K (128 bytes a row, 128-byte swizzle).
+// The scales travel as they lie in memory, in tiles of 128 rows x 4 blocks (512 bytes); each of the four warps writes them to its
+// own lane quarter (every quarter holds all 128 rows, 32 a column); a product takes 64 values of K and reads its scales there.
 //   M > 128   a pair of CTAs per 256 x BN tile (cta_group::2): each stages 128 rows of A, half of the B columns, the scales of its own
 //             rows and those of all columns (each multiplies its rows with all of them)
 //   M <= 128  one CTA, 128 x BN
-// Tensor memory: 512 columns = two accumulators and 64 columns of scales. Two accumulators of 256 columns leave no room, so they
-// overlap by 64 columns; the read-out takes those first and says so, and the next tile's products wait for that much only.
-// What bounds it: at 4.5 PFLOP/s and more the operands of a 256 x 256 tile (64 + 6 KB per 256 values of K and pair) come at what
-// L2 delivers to the whole chip, 5500 bytes a cycle; short K is bound by the read-out and by writing D.
+// Tensor memory: 512 columns = two accumulators and four sets of scales (24 columns each, nvfp4 48). Two accumulators of 256 columns
+// leave no room for that, so they overlap (by 96 and 192 columns); the read-out takes those first and says so, and the next tile's
+// products wait for that much only. (Copies run on meanwhile, and products are twice as fast as copies.)
+// What bounds it: at 4.5 PFLOP/s the operands of a 256 x 256 tile (64 + 6 KB, nvfp4 + 12 KB, per 256 values of K and pair) come at what
+// L2 delivers to the whole chip, 5500 to 6000 bytes a cycle; short K is bound by the read-out and by writing D.
 //
 // mx4_row_kernel, for up to eight rows of A: the weights are read once at memory speed, each code becomes two bytes by table
 // lookup (prmt), four products at a time are integer dot products (dp4a), a block's sum meets its scales in fp32.
@@ -27,19 +28,26 @@ namespace defl {
 namespace {
 
 constexpr int KB_ELEMENTS = 256, KB_BYTES = 128;
-constexpr int TC_THREADS = 320, TC_EPI_WARPS = 8;
+constexpr int TC_THREADS = 448, TC_EPI_WARPS = 8, SF_WARP = 10;
 constexpr int MAX_ST = 8;
 constexpr int STG_BYTES = 4096;                    // 32 rows x 128 bytes
-constexpr uint32_t SF_COL = 448;                   // tensor-memory columns of the scales: A's, then (16 further) B's
 constexpr uint32_t SMEM_MOST = 227 * 1024;
 
+// Tensor memory: SF_SETS sets of scales at the end, a stage each: A's four columns a tile, then those of up to two row tiles of B.
+// A set takes 1500 to 2300 cycles from the products that free it to those that read it again (a commit, a barrier in each CTA of
+// the pair, the copy, a barrier in the leader), so that two sets alone bounded a stage to 1060 cycles (mxfp4) and 1400.
+constexpr int SF_SETS = 4;
+__host__ __device__ constexpr uint32_t scale_set(int fmt) { return fmt == MXFP4 ? 24u : 48u; }
+__host__ __device__ constexpr uint32_t scale_column(int fmt) { return 512u - SF_SETS * scale_set(fmt); }
+
 struct TcParams4 {
-  CUtensorMap tmA, tmB, tmSA, tmSB, tmD;
+  CUtensorMap tmA, tmB, tmD;
+  const uint8_t* sa; const uint8_t* sb; int rt_a, rt_b, kt;      // tiles of scales: row tiles, tiles a row tile
   int M, N, batch, BN, b_shared;
   int tiles_m, tiles_n;
   int total_tiles;
   int kblocks, ksteps_last;                        // stages a tile, and products of 64 values in the last of them
-  int stages, nsb, overlap, stg_bufs;
+  int stages, overlap, stg_bufs;
   uint32_t a_bytes, b_bytes, sf_bytes, stage_bytes;
   uint32_t idesc;
   int out_f32, store_tma;
@@ -61,20 +69,22 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
       : "memory");
 }
 
-// 512 bytes of scales (32 rows of 16 bytes, no swizzle: groups of eight rows 128 bytes apart) to four columns of all lane quarters
-template <int PAIR>
-__device__ __forceinline__ void scales_to_tmem(uint32_t tcol, uint32_t saddr) {
-  const uint64_t desc = (uint64_t)((saddr >> 4) & 0x3FFFu) | (uint64_t)1 << 16 | (uint64_t)(128u >> 4) << 32 | (uint64_t)1 << 46;
-  if (PAIR) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tcol), "l"(desc) : "memory");
-  else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tcol), "l"(desc) : "memory");
+// Descriptors are put together from their halves; only the address in the low one changes.
+constexpr uint32_t OPERAND_HI = (1024u >> 4) | 1u << 14 | 2u << 29;      // groups of eight rows 1024 bytes apart, 128-byte swizzle
+__device__ __forceinline__ uint32_t desc_lo(uint32_t saddr) { return (saddr >> 4) | 1u << 16; }
+
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
 
 template <int FMT, int PAIR>
-__device__ __forceinline__ void umma4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
+__device__ __forceinline__ void umma4(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
 #define DEFL_MX4_MMA(GROUP, KIND)                                                                                    \
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"                                                     \
-               "tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], %1, %2, %3, [%4], [%5], p;\n\t}"               \
-               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory")
+  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %7, 0;\n\t"                                    \
+               "mov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"                                                    \
+               "tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], a, b, %4, [%5], [%6], p;\n\t}"                 \
+               ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(OPERAND_HI), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory")
   if (FMT == MXFP4) {
     if (PAIR) DEFL_MX4_MMA("2", "mxf4.block_scale.scale_vec::2X"); else DEFL_MX4_MMA("1", "mxf4.block_scale.scale_vec::2X");
   } else {
@@ -82,7 +92,6 @@ __device__ __forceinline__ void umma4(uint32_t d, uint64_t a, uint64_t b, uint32
   }
 #undef DEFL_MX4_MMA
 }
-
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap* tm, uint32_t src, int c0, int c1, int c2) {
   asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
                ::"l"(tm), "r"(src), "r"(c0), "r"(c1), "r"(c2) : "memory");
@@ -102,11 +111,15 @@ __device__ __forceinline__ Tile4 tile_of(const TcParams4& p, int tile) {
   return t;
 }
 
-template <int FMT, int PAIR>
+// NSB: 128-row tiles of scales that the B columns of a tile reach into
+template <int FMT, int PAIR, int NSB>
 __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_constant__ TcParams4 p) {
   constexpr int ATOMS = FMT == MXFP4 ? 2 : 4;      // tiles of scales a row tile and stage
+  constexpr uint32_t SF_SET = scale_set(FMT);
+  constexpr uint32_t SF_COL = scale_column(FMT);
+  const uint32_t acc1 = (uint32_t)(p.BN - p.overlap);
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t full_bar[MAX_ST], empty_bar[MAX_ST], acc_full_bar[2], acc_empty_bar[2], ovl_bar;
+  __shared__ __align__(8) uint64_t full_bar[MAX_ST], empty_bar[MAX_ST], land_bar[MAX_ST], acc_full_bar[2], acc_empty_bar[2], ovl_bar, sf_full_bar[SF_SETS], sf_empty_bar[SF_SETS];
   __shared__ uint32_t tmem_base_slot;
   __shared__ int abort_flag;
 
@@ -119,16 +132,15 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
   if (warp == 2 && lane == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&p.tmA) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&p.tmB) : "memory");
-    asm volatile("prefetch.tensormap [%0];" ::"l"(&p.tmSA) : "memory");
-    asm volatile("prefetch.tensormap [%0];" ::"l"(&p.tmSB) : "memory");
   }
   if (threadIdx.x == 0) {
     abort_flag = 0;
-    for (int s = 0; s < p.stages; ++s) { mbar_init(smem_u32(&full_bar[s]), 1); mbar_init(smem_u32(&empty_bar[s]), 1); }
+    for (int s = 0; s < p.stages; ++s) { mbar_init(smem_u32(&full_bar[s]), 1); mbar_init(smem_u32(&empty_bar[s]), 1); mbar_init(smem_u32(&land_bar[s]), 1); }
     for (int a = 0; a < 2; ++a) {
       mbar_init(smem_u32(&acc_full_bar[a]), 1);
       mbar_init(smem_u32(&acc_empty_bar[a]), (PAIR ? 2 : 1) * TC_EPI_WARPS);
     }
+    for (int a = 0; a < SF_SETS; ++a) { mbar_init(smem_u32(&sf_full_bar[a]), (PAIR ? 2 : 1) * 4); mbar_init(smem_u32(&sf_empty_bar[a]), 1); }
     mbar_init(smem_u32(&ovl_bar), (PAIR ? 2 : 1) * TC_EPI_WARPS);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -146,18 +158,15 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
 
   if (warp == 0) {
     // ------------------------------------------------------------------ copies: every lane of the step's issues one
-    const uint32_t full0 = smem_u32(&full_bar[0]), empty0 = smem_u32(&empty_bar[0]);
+    // The codes of a pair count on the leader's barrier, where the products wait for them; scales on one of each CTA's own.
+    const uint32_t full0 = smem_u32(&full_bar[0]), empty0 = smem_u32(&empty_bar[0]), land0 = smem_u32(&land_bar[0]);
     const uint32_t full0_sig = PAIR ? map_to_cta(full0, 0) : full0;
-    const uint32_t tx = (PAIR ? 2u : 1u) * p.stage_bytes;
-    constexpr int XS = ATOMS / 2;                  // boxes of 1024 bytes of scales a row tile and stage
-    // lane 0: A, 1: B, then A's scales, then B's
-    const int idx = lane - 2;
-    const bool is_sa = idx >= 0 && idx < XS, is_sb = idx >= XS && idx < XS * (1 + p.nsb);
-    const int sb_rt = is_sb ? (idx - XS) / XS : 0, part = is_sa ? idx : is_sb ? (idx - XS) % XS : 0;
-    const bool on = lane < 2 || is_sa || is_sb;
-    const CUtensorMap* tm = lane == 0 ? &p.tmA : lane == 1 ? &p.tmB : is_sa ? &p.tmSA : &p.tmSB;
-    const uint32_t off = lane == 0 ? 0u : lane == 1 ? p.a_bytes
-                         : p.a_bytes + p.b_bytes + (is_sa ? 0u : (uint32_t)(1 + sb_rt) * p.sf_bytes) + (uint32_t)part * 1024u;
+    const uint32_t tx = (PAIR ? 2u : 1u) * (p.a_bytes + p.b_bytes);
+    // lane 0: A, 1: B, 2: A's scales, then B's, a row tile a lane. Scales are contiguous and go as plain bulk copies (as boxes of a
+    // tensor without swizzle they came at 16 bytes a cycle: a stage took 1075 cycles, nvfp4 1417).
+    const bool is_scale = lane >= 2 && lane < 3 + NSB;
+    const CUtensorMap* tm = lane == 0 ? &p.tmA : &p.tmB;
+    const uint32_t off = lane == 0 ? 0u : lane == 1 ? p.a_bytes : p.a_bytes + p.b_bytes + (uint32_t)(lane - 2) * p.sf_bytes;
     uint32_t stage = 0, phase = 0;
     bool live = true;
     pdl_wait();
@@ -165,18 +174,31 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
       const Tile4 t = tile_of<PAIR>(p, tile);
       const int n0 = t.tn * p.BN, m0 = t.tm * TILE_M + (int)rank * 128;
       const int bz_b = p.b_shared ? 0 : t.bz;
-      const int c1 = lane == 0 ? m0 : lane == 1 ? n0 + (PAIR ? (int)rank * (t.n_eff >> 1) : 0) : is_sa ? m0 >> 7 : (n0 >> 7) + sb_rt;
-      const int c2 = (lane == 0 || is_sa) ? t.bz : bz_b;
+      const int c1 = lane == 0 ? m0 : n0 + (PAIR ? (int)rank * (t.n_eff >> 1) : 0), c2 = lane == 0 ? t.bz : bz_b;
+      // row tiles that do not exist are not copied: what their place holds meets rows and columns that are not stored
+      const int rt = lane == 2 ? m0 >> 7 : (n0 >> 7) + lane - 3;
+      const bool exists = is_scale && rt < (lane == 2 ? p.rt_a : p.rt_b);
+      const uint8_t* src = nullptr;
+      if (exists) src = (lane == 2 ? p.sa : p.sb) + ((long long)(lane == 2 ? t.bz : bz_b) * (lane == 2 ? p.rt_a : p.rt_b) + rt) * p.kt * 512;
+      const uint32_t count = (uint32_t)__popc(__ballot_sync(0xffffffffu, exists));
       for (int kb = 0; kb < p.kblocks; ++kb) {
+        const uint32_t sf_now = (uint32_t)min(ATOMS, p.kt - kb * ATOMS) * 512u;
         int ok = 1;
         if (lane == 0) ok = mbar_wait(empty0 + 8u * stage, phase ^ 1u, &abort_flag, p.status, p.wait_ns) ? 1 : 0;
         ok = __shfl_sync(0xffffffffu, ok, 0);
         if (!ok) { live = false; break; }
-        if (lane == 0 && rank == 0) mbar_expect_tx(full0 + 8u * stage, tx);
-        if (on) {
-          const uint32_t dst = smem_base + stage * p.stage_bytes + off, bar = full0_sig + 8u * stage;
-          const int c0 = lane < 2 ? kb * KB_BYTES : kb * (ATOMS * 128) + part * 256;
-          if (PAIR) tma_load_3d_pair(dst, tm, bar, c0, c1, c2); else tma_load_3d(dst, tm, bar, c0, c1, c2);
+        if (lane == 0) {
+          if (rank == 0) mbar_expect_tx(full0 + 8u * stage, tx);
+          mbar_expect_tx(land0 + 8u * stage, count * sf_now);
+        }
+        __syncwarp();
+        const uint32_t dst = smem_base + stage * p.stage_bytes + off;
+        if (lane < 2) {
+          if (PAIR) tma_load_3d_pair(dst, tm, full0_sig + 8u * stage, kb * KB_BYTES, c1, c2);
+          else tma_load_3d(dst, tm, full0 + 8u * stage, kb * KB_BYTES, c1, c2);
+        } else if (exists) {
+          asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                       ::"r"(dst), "l"(src + (long long)kb * (ATOMS * 512)), "r"(sf_now), "r"(land0 + 8u * stage) : "memory");
         }
         __syncwarp();
         if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
@@ -185,11 +207,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
   } else if (warp == 1) {
     // ------------------------------------------------------------------ products
     if (lane == 0 && rank == 0) {
-      const uint64_t hi = smem_desc_hi(16u, 1024u);
-      const uint32_t full0 = smem_u32(&full_bar[0]), empty0 = smem_u32(&empty_bar[0]);
-      const uint32_t acc1 = p.overlap ? SF_COL - 256u : 256u;
-      const uint32_t sa_col = tmem_base + SF_COL, sb_col = tmem_base + SF_COL + 16u;
-      uint32_t stage = 0, phase = 0;
+      const uint32_t full0 = smem_u32(&full_bar[0]), empty0 = smem_u32(&empty_bar[0]), sf_full0 = smem_u32(&sf_full_bar[0]), sf_empty0 = smem_u32(&sf_empty_bar[0]);
+      const uint32_t sf_col = tmem_base + SF_COL, b_off = p.a_bytes >> 4;
+      uint32_t stage = 0, phase = 0, set = 0, set_phase = 0;
       pdl_wait();
       for (int tile = tile0, it = 0; tile < p.total_tiles; tile += tile_step, ++it) {
         const Tile4 t = tile_of<PAIR>(p, tile);
@@ -200,38 +220,70 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
         const uint32_t d = tmem_base + (acc ? acc1 : 0u);
         const uint32_t idesc = p.idesc | ((uint32_t)(t.n_eff >> 3) << 17);
         const uint32_t shift = (uint32_t)((t.tn * p.BN) & 127) >> 5;      // B's first row within its tile of scales, in columns
-        bool ok = true;
-        for (int kb = 0; kb < p.kblocks; ++kb) {
-          if (!mbar_wait(full0 + 8u * stage, phase, &abort_flag, p.status, p.wait_ns)) { ok = false; break; }
+        int kb = 0;
+        for (; kb < p.kblocks; ++kb) {
+          if (!mbar_wait(full0 + 8u * stage, phase, &abort_flag, p.status, p.wait_ns)) break;
+          if (!mbar_wait(sf_full0 + 8u * set, set_phase, &abort_flag, p.status, p.wait_ns)) break;
           tc_fence_after();
-          const uint32_t sA = smem_base + stage * p.stage_bytes, sB = sA + p.a_bytes, sS = sB + p.b_bytes;
+          const uint32_t lo = desc_lo(smem_base + stage * p.stage_bytes), sa = sf_col + set * SF_SET, sb = sa + ATOMS * 4u + shift;
           const int ksteps = kb + 1 < p.kblocks ? 4 : p.ksteps_last;
 #pragma unroll
-          for (int a = 0; a < ATOMS; ++a) {
-            if (a * (4 / ATOMS) >= ksteps) break;
-            scales_to_tmem<PAIR>(sa_col + 4u * a, sS + 512u * a);
-            for (int r = 0; r < p.nsb; ++r) scales_to_tmem<PAIR>(sb_col + 4u * (uint32_t)(a * p.nsb + r), sS + (uint32_t)(1 + r) * p.sf_bytes + 512u * a);
-          }
-#pragma unroll
           for (int kk = 0; kk < 4; ++kk) {
-            if (kk >= ksteps) break;
-            const int a = FMT == MXFP4 ? kk >> 1 : kk;
-            const uint32_t id = FMT == MXFP4 ? (uint32_t)(kk & 1) * 2u : 0u;
-            umma4<FMT, PAIR>(d, hi | (uint64_t)((sA >> 4) + 2u * kk), hi | (uint64_t)((sB >> 4) + 2u * kk), idesc | id << 4 | id << 29,
-                             sa_col + 4u * a, sb_col + 4u * (uint32_t)(a * p.nsb) + shift, (kb | kk) ? 1u : 0u);
+            if (kk < ksteps) {
+              const int a = FMT == MXFP4 ? kk >> 1 : kk;
+              const uint32_t id = FMT == MXFP4 ? (uint32_t)(kk & 1) * 2u : 0u;
+              umma4<FMT, PAIR>(d, lo + 2u * kk, lo + b_off + 2u * kk, idesc | id << 4 | id << 29, sa + 4u * a, sb + 4u * (a * NSB), (kb | kk) ? 1u : 0u);
+            }
           }
-          if (PAIR) umma_commit_pair(empty0 + 8u * stage); else umma_commit(empty0 + 8u * stage);
+          if (PAIR) { umma_commit_pair(empty0 + 8u * stage); umma_commit_pair(sf_empty0 + 8u * set); }
+          else { umma_commit(empty0 + 8u * stage); umma_commit(sf_empty0 + 8u * set); }
           if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
+          if (++set == SF_SETS) { set = 0; set_phase ^= 1u; }
         }
-        if (!ok) break;
+        if (kb < p.kblocks) break;
         if (PAIR) umma_commit_pair(smem_u32(&acc_full_bar[acc])); else umma_commit(smem_u32(&acc_full_bar[acc]));
+      }
+    }
+  } else if (warp >= SF_WARP) {
+    // ------------------------------------------------------------------ scales: from each stage to tensor memory, a stage ahead of the
+    // products. By register and not with tcgen05.cp: that moves 512 bytes in 45 to 120 cycles, six or twelve of them a stage, in the
+    // same queue as the products (8192 x 1600 x 6400: 76 us mxfp4, 106 nvfp4; issued by a warp of its own 56 and 75).
+    const uint32_t land0 = smem_u32(&land_bar[0]), sf_empty0 = smem_u32(&sf_empty_bar[0]);
+    const uint32_t sf_full0 = PAIR ? map_to_cta(smem_u32(&sf_full_bar[0]), 0) : smem_u32(&sf_full_bar[0]);
+    const uint32_t sf_col = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + SF_COL, s_off = p.a_bytes + p.b_bytes + 16u * lane;
+    uint32_t stage = 0, phase = 0, set = 0, set_phase = 0;
+    bool live = true;
+    pdl_wait();
+    for (int tile = tile0; tile < p.total_tiles && live; tile += tile_step) {
+      for (int kb = 0; kb < p.kblocks; ++kb) {
+        const bool ok = mbar_wait(land0 + 8u * stage, phase, &abort_flag, p.status, p.wait_ns) &&
+                        mbar_wait(sf_empty0 + 8u * set, set_phase ^ 1u, &abort_flag, p.status, p.wait_ns);
+        if (!__all_sync(0xffffffffu, ok)) { live = false; break; }
+        tc_fence_after();
+        const uint32_t src = smem_base + stage * p.stage_bytes + s_off;
+        uint32_t v[ATOMS * 4 * (1 + NSB)];
+        // columns: A's four a tile, then B's, the row tiles of one K position side by side
+#pragma unroll
+        for (int i = 0; i < ATOMS * (1 + NSB); ++i) {
+          const int a = i < ATOMS ? i : (i - ATOMS) / NSB, r = i < ATOMS ? 0 : 1 + (i - ATOMS) % NSB;
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[4 * i]), "=r"(v[4 * i + 1]), "=r"(v[4 * i + 2]), "=r"(v[4 * i + 3])
+                       : "r"(src + (uint32_t)r * (ATOMS * 512u) + 512u * a) : "memory");
+        }
+        const uint32_t dst = sf_col + set * SF_SET;
+#pragma unroll
+        for (int i = 0; i < ATOMS * (1 + NSB) / 2; ++i) tmem_st8(dst + 8u * i, v + 8 * i);
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) { if (PAIR) mbar_arrive_cluster(sf_full0 + 8u * set); else mbar_arrive(sf_full0 + 8u * set); }
+        if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
+        if (++set == SF_SETS) { set = 0; set_phase ^= 1u; }
       }
     }
   } else {
     // ------------------------------------------------------------------ read-out: 32 rows and every other chunk of columns a warp
     const int q = warp & 3, wsel = (warp - 2) >> 2;
     const uint32_t stg0 = smem_base + (uint32_t)p.stages * p.stage_bytes + (uint32_t)((warp - 2) * p.stg_bufs) * STG_BYTES;
-    const uint32_t acc1 = p.overlap ? SF_COL - 256u : 256u;
     const uint32_t ovl_sig = PAIR ? map_to_cta(smem_u32(&ovl_bar), 0) : smem_u32(&ovl_bar);
     const int cw = p.out_f32 ? 32 : 64;            // columns of 128 bytes
     int buf = 0;
@@ -245,7 +297,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
       tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (acc ? acc1 : 0u);
       const int row0 = t.tm * TILE_M + (int)rank * 128 + q * 32, n0 = t.tn * p.BN;
-      const int chunks = (t.n_eff + cw - 1) / cw, ovl_chunks = 64 / cw, full = p.BN / cw;
+      const int chunks = (t.n_eff + cw - 1) / cw, ovl_chunks = (p.overlap + cw - 1) / cw, full = p.BN / cw;
       bool told = !p.overlap;
       // the overlapping columns come first: the last ones of the first accumulator, the first ones of the second
       for (int i = wsel; i < full; i += 2) {
@@ -472,14 +524,14 @@ EncodeFn encode_fn() {
   return fn;
 }
 
-// [batch, rows, inner] of elements of `es` bytes, boxes of box_inner x box_rows
+// [batch, rows, inner], boxes of box_inner x box_rows, 128 bytes wide and swizzled
 bool encode(CUtensorMap* tm, CUtensorMapDataType type, const void* base, long long inner, long long rows, long long batch, long long row_bytes,
-            long long batch_bytes, uint32_t box_inner, uint32_t box_rows, bool swizzle) {
+            long long batch_bytes, uint32_t box_inner, uint32_t box_rows) {
   const cuuint64_t dims[3] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)batch};
   const cuuint64_t strides[2] = {(cuuint64_t)row_bytes, (cuuint64_t)batch_bytes};
   const cuuint32_t box[3] = {box_inner, box_rows, 1}, est[3] = {1, 1, 1};
   return encode_fn()(tm, type, 3, const_cast<void*>(base), dims, strides, box, est, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                     swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -507,7 +559,7 @@ int choose_width(const Mx4Gemm& g, bool pair, int num_sms) {
   return best;
 }
 
-template <int FMT, int PAIR>
+template <int FMT, int PAIR, int NSB>
 cudaError_t tc_start(const TcParams4& p, int grid, size_t smem, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
@@ -517,7 +569,7 @@ cudaError_t tc_start(const TcParams4& p, int grid, size_t smem, cudaStream_t st)
   attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(TC_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = st;
   cfg.attrs = attr; cfg.numAttrs = PAIR ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, mx4_tc_kernel<FMT, PAIR>, p);
+  return cudaLaunchKernelEx(&cfg, mx4_tc_kernel<FMT, PAIR, NSB>, p);
 }
 
 template <int FMT, int T>
@@ -536,12 +588,23 @@ cudaError_t row_pick(const RowParams& p, int b, int num_sms, cudaStream_t st) {
 
 }  // namespace
 
+namespace {
+template <int FMT, int PAIR>
+cudaError_t tc_limit() {
+  const cudaError_t e = cudaFuncSetAttribute(mx4_tc_kernel<FMT, PAIR, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST - 1024);
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(mx4_tc_kernel<FMT, PAIR, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST - 1024);
+}
+template <int FMT>
+cudaError_t tc_pick(const TcParams4& p, bool pair, int nsb, int grid, size_t smem, cudaStream_t st) {
+  if (pair) return nsb == 1 ? tc_start<FMT, 1, 1>(p, grid, smem, st) : tc_start<FMT, 1, 2>(p, grid, smem, st);
+  return nsb == 1 ? tc_start<FMT, 0, 1>(p, grid, smem, st) : tc_start<FMT, 0, 2>(p, grid, smem, st);
+}
+}  // namespace
+
 cudaError_t mx4_gemm_prepare() {
   cudaError_t e;
-  if ((e = cudaFuncSetAttribute(mx4_tc_kernel<MXFP4, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST - 1024)) != cudaSuccess) return e;
-  if ((e = cudaFuncSetAttribute(mx4_tc_kernel<MXFP4, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST - 1024)) != cudaSuccess) return e;
-  if ((e = cudaFuncSetAttribute(mx4_tc_kernel<NVFP4, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST - 1024)) != cudaSuccess) return e;
-  return cudaFuncSetAttribute(mx4_tc_kernel<NVFP4, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST - 1024);
+  if ((e = tc_limit<MXFP4, 0>()) != cudaSuccess || (e = tc_limit<MXFP4, 1>()) != cudaSuccess || (e = tc_limit<NVFP4, 0>()) != cudaSuccess) return e;
+  return tc_limit<NVFP4, 1>();
 }
 
 cudaError_t mx4_gemm_launch(const Mx4Gemm& g, cudaStream_t st, int* status, int num_sms, unsigned long long wait_ns, long long* launches) {
@@ -562,14 +625,14 @@ cudaError_t mx4_gemm_launch(const Mx4Gemm& g, cudaStream_t st, int* status, int 
   const long long total = (long long)p.tiles_m * p.tiles_n * g.b;
   if (total > 0x3fffffff) return cudaErrorInvalidValue;
   p.total_tiles = (int)total;
-  const int width = mx4_width(g.K), kt = mx4_scale_tiles(g.K, g.fmt), atoms = g.fmt == MXFP4 ? 2 : 4;
+  const int width = mx4_width(g.K), atoms = g.fmt == MXFP4 ? 2 : 4;
   p.kblocks = (width + KB_ELEMENTS - 1) / KB_ELEMENTS;
   p.ksteps_last = (width - (p.kblocks - 1) * KB_ELEMENTS + 63) / 64;
-  p.nsb = p.BN <= 128 ? 1 : 2;
-  p.overlap = p.BN == 256;
+  const int nsb = p.BN <= 128 ? 1 : 2;
+  p.overlap = 2 * p.BN > (int)scale_column(g.fmt) ? 2 * p.BN - (int)scale_column(g.fmt) : 0;
   const uint32_t b_rows = (uint32_t)(pair ? p.BN / 2 : p.BN);
   p.a_bytes = 128 * KB_BYTES; p.b_bytes = b_rows * KB_BYTES; p.sf_bytes = (uint32_t)atoms * 512u;
-  p.stage_bytes = p.a_bytes + p.b_bytes + (uint32_t)(1 + p.nsb) * p.sf_bytes;
+  p.stage_bytes = p.a_bytes + p.b_bytes + (uint32_t)(1 + nsb) * p.sf_bytes;
   p.stg_bufs = 2;
   const uint32_t stg = (uint32_t)(TC_EPI_WARPS * p.stg_bufs) * STG_BYTES, room = SMEM_MOST - 1024 - 1024 - stg;
   p.stages = (int)(room / p.stage_bytes);
@@ -585,21 +648,18 @@ cudaError_t mx4_gemm_launch(const Mx4Gemm& g, cudaStream_t st, int* status, int 
   // (whole rows of 16-byte pieces: the copy engine writes the last piece in full, past a row that ends inside it)
   p.store_tma = (reinterpret_cast<uintptr_t>(g.D) & 15u) == 0 && (g.N * es) % 16 == 0 && (g.ldd * es) % 16 == 0 && (g.b == 1 || (g.batch_d * es) % 16 == 0);
   const int bb = g.b_shared ? 1 : g.b;
-  const long long rta = mx4_row_tiles(g.M), rtb = mx4_row_tiles(g.N);
-  bool ok = encode(&p.tmA, CU_TENSOR_MAP_DATA_TYPE_UINT8, g.A.codes, width / 2, g.M, g.b, width / 2, (long long)g.M * (width / 2), KB_BYTES, 128, true) &&
-            encode(&p.tmB, CU_TENSOR_MAP_DATA_TYPE_UINT8, g.B.codes, width / 2, g.N, bb, width / 2, (long long)g.N * (width / 2), KB_BYTES, b_rows, true) &&
-            encode(&p.tmSA, CU_TENSOR_MAP_DATA_TYPE_UINT32, g.A.scales, kt * 128ll, rta, g.b, kt * 512ll, rta * kt * 512ll, 256, 1, false) &&
-            encode(&p.tmSB, CU_TENSOR_MAP_DATA_TYPE_UINT32, g.B.scales, kt * 128ll, rtb, bb, kt * 512ll, rtb * kt * 512ll, 256, 1, false);
+  bool ok = encode(&p.tmA, CU_TENSOR_MAP_DATA_TYPE_UINT8, g.A.codes, width / 2, g.M, g.b, width / 2, (long long)g.M * (width / 2), KB_BYTES, 128) &&
+            encode(&p.tmB, CU_TENSOR_MAP_DATA_TYPE_UINT8, g.B.codes, width / 2, g.N, bb, width / 2, (long long)g.N * (width / 2), KB_BYTES, b_rows);
+  p.sa = g.A.scales; p.sb = g.B.scales; p.rt_a = mx4_row_tiles(g.M); p.rt_b = mx4_row_tiles(g.N); p.kt = mx4_scale_tiles(g.K, g.fmt);
   if (ok && p.store_tma) {
     const long long batch_bytes = g.b > 1 ? g.batch_d * es : g.ldd * es * g.M;
     ok = encode(&p.tmD, p.out_f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, g.D, g.N, g.M, g.b, g.ldd * es, batch_bytes,
-                p.out_f32 ? 32 : 64, 32, true);
+                p.out_f32 ? 32 : 64, 32);
   }
   if (!ok) return cudaErrorInvalidValue;
   const int slots = pair ? num_sms / 2 : num_sms, runs = p.total_tiles < slots ? p.total_tiles : slots, grid = pair ? 2 * runs : runs;
   if (launches) ++*launches;
-  if (g.fmt == MXFP4) return pair ? tc_start<MXFP4, 1>(p, grid, smem, st) : tc_start<MXFP4, 0>(p, grid, smem, st);
-  return pair ? tc_start<NVFP4, 1>(p, grid, smem, st) : tc_start<NVFP4, 0>(p, grid, smem, st);
+  return g.fmt == MXFP4 ? tc_pick<MXFP4>(p, pair, nsb, grid, smem, st) : tc_pick<NVFP4>(p, pair, nsb, grid, smem, st);
 }
 
 }  // namespace defl

@@ -28,15 +28,14 @@ namespace defl {
 namespace {
 
 constexpr int KB_ELEMENTS = 256, KB_BYTES = 128;
-constexpr int TC_THREADS = 448, TC_EPI_WARPS = 8, SF_WARP = 10;
+constexpr int TC_THREADS = 480, TC_EPI_WARPS = 8, SF_WARP = 10;
 constexpr int MAX_ST = 8;
 constexpr int STG_BYTES = 4096;                    // 32 rows x 128 bytes
 constexpr uint32_t SMEM_MOST = 227 * 1024;
 
 // Tensor memory: SF_SETS sets of scales at the end, a stage each: A's four columns a tile, then those of up to two row tiles of B.
-// A set takes 1500 to 2300 cycles from the products that free it to those that read it again (a commit, a barrier in each CTA of
-// the pair, the copy, a barrier in the leader), so that two sets alone bounded a stage to 1060 cycles (mxfp4) and 1400.
 constexpr int SF_SETS = 4;
+__host__ __device__ constexpr int scale_ring(int fmt) { return fmt == MXFP4 ? 8 : 5; }      // slots in shared memory
 __host__ __device__ constexpr uint32_t scale_set(int fmt) { return fmt == MXFP4 ? 24u : 48u; }
 __host__ __device__ constexpr uint32_t scale_column(int fmt) { return 512u - SF_SETS * scale_set(fmt); }
 
@@ -47,8 +46,8 @@ struct TcParams4 {
   int tiles_m, tiles_n;
   int total_tiles;
   int kblocks, ksteps_last;                        // stages a tile, and products of 64 values in the last of them
-  int stages, overlap, stg_bufs;
-  uint32_t a_bytes, b_bytes, sf_bytes, stage_bytes;
+  int stages, sets, overlap, stg_bufs;
+  uint32_t a_bytes, b_bytes, stage_bytes;
   uint32_t idesc;
   int out_f32, store_tma;
   void* D; long long ldd, batch_d;
@@ -117,9 +116,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
   constexpr int ATOMS = FMT == MXFP4 ? 2 : 4;      // tiles of scales a row tile and stage
   constexpr uint32_t SF_SET = scale_set(FMT);
   constexpr uint32_t SF_COL = scale_column(FMT);
+  constexpr int SF_RING = scale_ring(FMT);
   const uint32_t acc1 = (uint32_t)(p.BN - p.overlap);
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t full_bar[MAX_ST], empty_bar[MAX_ST], land_bar[MAX_ST], acc_full_bar[2], acc_empty_bar[2], ovl_bar, sf_full_bar[SF_SETS], sf_empty_bar[SF_SETS];
+  __shared__ __align__(8) uint64_t full_bar[MAX_ST], empty_bar[MAX_ST], land_bar[SF_RING], slot_empty_bar[SF_RING], acc_full_bar[2], acc_empty_bar[2], ovl_bar;
   __shared__ uint32_t tmem_base_slot;
   __shared__ int abort_flag;
 
@@ -135,12 +135,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
   }
   if (threadIdx.x == 0) {
     abort_flag = 0;
-    for (int s = 0; s < p.stages; ++s) { mbar_init(smem_u32(&full_bar[s]), 1); mbar_init(smem_u32(&empty_bar[s]), 1); mbar_init(smem_u32(&land_bar[s]), 1); }
+    // (a stage is full when its codes are here and four warps, of each CTA, have its scales in tensor memory)
+    for (int s = 0; s < p.stages; ++s) { mbar_init(smem_u32(&full_bar[s]), 1 + (PAIR ? 2 : 1) * 4); mbar_init(smem_u32(&empty_bar[s]), 1); }
+    for (int s = 0; s < SF_RING; ++s) { mbar_init(smem_u32(&land_bar[s]), 1); mbar_init(smem_u32(&slot_empty_bar[s]), 4); }
     for (int a = 0; a < 2; ++a) {
       mbar_init(smem_u32(&acc_full_bar[a]), 1);
       mbar_init(smem_u32(&acc_empty_bar[a]), (PAIR ? 2 : 1) * TC_EPI_WARPS);
     }
-    for (int a = 0; a < SF_SETS; ++a) { mbar_init(smem_u32(&sf_full_bar[a]), (PAIR ? 2 : 1) * 4); mbar_init(smem_u32(&sf_empty_bar[a]), 1); }
     mbar_init(smem_u32(&ovl_bar), (PAIR ? 2 : 1) * TC_EPI_WARPS);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -157,16 +158,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
   pdl_launch();
 
   if (warp == 0) {
-    // ------------------------------------------------------------------ copies: every lane of the step's issues one
-    // The codes of a pair count on the leader's barrier, where the products wait for them; scales on one of each CTA's own.
-    const uint32_t full0 = smem_u32(&full_bar[0]), empty0 = smem_u32(&empty_bar[0]), land0 = smem_u32(&land_bar[0]);
+    // ------------------------------------------------------------------ copies of the codes: A by lane 0, B by lane 1. Those of a pair
+    // count on the leader's barrier, where the products wait for them.
+    const uint32_t full0 = smem_u32(&full_bar[0]), empty0 = smem_u32(&empty_bar[0]);
     const uint32_t full0_sig = PAIR ? map_to_cta(full0, 0) : full0;
     const uint32_t tx = (PAIR ? 2u : 1u) * (p.a_bytes + p.b_bytes);
-    // lane 0: A, 1: B, 2: A's scales, then B's, a row tile a lane. Scales are contiguous and go as plain bulk copies (as boxes of a
-    // tensor without swizzle they came at 16 bytes a cycle: a stage took 1075 cycles, nvfp4 1417).
-    const bool is_scale = lane >= 2 && lane < 3 + NSB;
     const CUtensorMap* tm = lane == 0 ? &p.tmA : &p.tmB;
-    const uint32_t off = lane == 0 ? 0u : lane == 1 ? p.a_bytes : p.a_bytes + p.b_bytes + (uint32_t)(lane - 2) * p.sf_bytes;
+    const uint32_t off = lane == 0 ? 0u : p.a_bytes;
     uint32_t stage = 0, phase = 0;
     bool live = true;
     pdl_wait();
@@ -175,30 +173,16 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
       const int n0 = t.tn * p.BN, m0 = t.tm * TILE_M + (int)rank * 128;
       const int bz_b = p.b_shared ? 0 : t.bz;
       const int c1 = lane == 0 ? m0 : n0 + (PAIR ? (int)rank * (t.n_eff >> 1) : 0), c2 = lane == 0 ? t.bz : bz_b;
-      // row tiles that do not exist are not copied: what their place holds meets rows and columns that are not stored
-      const int rt = lane == 2 ? m0 >> 7 : (n0 >> 7) + lane - 3;
-      const bool exists = is_scale && rt < (lane == 2 ? p.rt_a : p.rt_b);
-      const uint8_t* src = nullptr;
-      if (exists) src = (lane == 2 ? p.sa : p.sb) + ((long long)(lane == 2 ? t.bz : bz_b) * (lane == 2 ? p.rt_a : p.rt_b) + rt) * p.kt * 512;
-      const uint32_t count = (uint32_t)__popc(__ballot_sync(0xffffffffu, exists));
       for (int kb = 0; kb < p.kblocks; ++kb) {
-        const uint32_t sf_now = (uint32_t)min(ATOMS, p.kt - kb * ATOMS) * 512u;
         int ok = 1;
         if (lane == 0) ok = mbar_wait(empty0 + 8u * stage, phase ^ 1u, &abort_flag, p.status, p.wait_ns) ? 1 : 0;
         ok = __shfl_sync(0xffffffffu, ok, 0);
         if (!ok) { live = false; break; }
-        if (lane == 0) {
-          if (rank == 0) mbar_expect_tx(full0 + 8u * stage, tx);
-          mbar_expect_tx(land0 + 8u * stage, count * sf_now);
-        }
-        __syncwarp();
-        const uint32_t dst = smem_base + stage * p.stage_bytes + off;
+        if (lane == 0 && rank == 0) mbar_expect_tx(full0 + 8u * stage, tx);
         if (lane < 2) {
+          const uint32_t dst = smem_base + stage * p.stage_bytes + off;
           if (PAIR) tma_load_3d_pair(dst, tm, full0_sig + 8u * stage, kb * KB_BYTES, c1, c2);
           else tma_load_3d(dst, tm, full0 + 8u * stage, kb * KB_BYTES, c1, c2);
-        } else if (exists) {
-          asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                       ::"r"(dst), "l"(src + (long long)kb * (ATOMS * 512)), "r"(sf_now), "r"(land0 + 8u * stage) : "memory");
         }
         __syncwarp();
         if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
@@ -207,9 +191,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
   } else if (warp == 1) {
     // ------------------------------------------------------------------ products
     if (lane == 0 && rank == 0) {
-      const uint32_t full0 = smem_u32(&full_bar[0]), empty0 = smem_u32(&empty_bar[0]), sf_full0 = smem_u32(&sf_full_bar[0]), sf_empty0 = smem_u32(&sf_empty_bar[0]);
+      const uint32_t full0 = smem_u32(&full_bar[0]), empty0 = smem_u32(&empty_bar[0]);
       const uint32_t sf_col = tmem_base + SF_COL, b_off = p.a_bytes >> 4;
-      uint32_t stage = 0, phase = 0, set = 0, set_phase = 0;
+      uint32_t stage = 0, phase = 0, set = 0, ready = 0;
       pdl_wait();
       for (int tile = tile0, it = 0; tile < p.total_tiles; tile += tile_step, ++it) {
         const Tile4 t = tile_of<PAIR>(p, tile);
@@ -222,9 +206,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
         const uint32_t shift = (uint32_t)((t.tn * p.BN) & 127) >> 5;      // B's first row within its tile of scales, in columns
         int kb = 0;
         for (; kb < p.kblocks; ++kb) {
-          if (!mbar_wait(full0 + 8u * stage, phase, &abort_flag, p.status, p.wait_ns)) break;
-          if (!mbar_wait(sf_full0 + 8u * set, set_phase, &abort_flag, p.status, p.wait_ns)) break;
+          if (!ready && !mbar_wait(full0 + 8u * stage, phase, &abort_flag, p.status, p.wait_ns)) break;
           tc_fence_after();
+          // a look at the next stage's barrier now: a wait takes 170 cycles also where there is nothing to wait for, and this thread's
+          // time is what bounded the kernel (two such waits and the products: 840 cycles a stage)
+          ready = stage + 1 == (uint32_t)p.stages ? mbar_test(full0, phase ^ 1u) : mbar_test(full0 + 8u * (stage + 1), phase);
           const uint32_t lo = desc_lo(smem_base + stage * p.stage_bytes), sa = sf_col + set * SF_SET, sb = sa + ATOMS * 4u + shift;
           const int ksteps = kb + 1 < p.kblocks ? 4 : p.ksteps_last;
 #pragma unroll
@@ -235,39 +221,73 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
               umma4<FMT, PAIR>(d, lo + 2u * kk, lo + b_off + 2u * kk, idesc | id << 4 | id << 29, sa + 4u * a, sb + 4u * (a * NSB), (kb | kk) ? 1u : 0u);
             }
           }
-          if (PAIR) { umma_commit_pair(empty0 + 8u * stage); umma_commit_pair(sf_empty0 + 8u * set); }
-          else { umma_commit(empty0 + 8u * stage); umma_commit(sf_empty0 + 8u * set); }
+          // (one commit a stage, for its codes and its scales: a second one to both CTAs took 250 cycles)
+          if (PAIR) umma_commit_pair(empty0 + 8u * stage); else umma_commit(empty0 + 8u * stage);
           if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
-          if (++set == SF_SETS) { set = 0; set_phase ^= 1u; }
+          if (++set == (uint32_t)p.sets) set = 0;
         }
         if (kb < p.kblocks) break;
         if (PAIR) umma_commit_pair(smem_u32(&acc_full_bar[acc])); else umma_commit(smem_u32(&acc_full_bar[acc]));
       }
     }
   } else if (warp >= SF_WARP) {
-    // ------------------------------------------------------------------ scales: from each stage to tensor memory, a stage ahead of the
-    // products. By register and not with tcgen05.cp: that moves 512 bytes in 45 to 120 cycles, six or twelve of them a stage, in the
-    // same queue as the products (8192 x 1600 x 6400: 76 us mxfp4, 106 nvfp4; issued by a warp of its own 56 and 75).
-    const uint32_t land0 = smem_u32(&land_bar[0]), sf_empty0 = smem_u32(&sf_empty_bar[0]);
-    const uint32_t sf_full0 = PAIR ? map_to_cta(smem_u32(&sf_full_bar[0]), 0) : smem_u32(&sf_full_bar[0]);
-    const uint32_t sf_col = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + SF_COL, s_off = p.a_bytes + p.b_bytes + 16u * lane;
-    uint32_t stage = 0, phase = 0, set = 0, set_phase = 0;
+    // ------------------------------------------------------------------ scales: from memory through a ring of their own to tensor memory,
+    // stages ahead of the codes, so that the products wait for codes alone. By register and not with tcgen05.cp: that moves 512
+    // bytes in 45 to 120 cycles, six or twelve of them a stage, in the same queue as the products. Plain bulk copies: as boxes of a
+    // tensor without swizzle they came at 16 bytes a cycle.
+    const uint32_t land0 = smem_u32(&land_bar[0]), slot_empty0 = smem_u32(&slot_empty_bar[0]), empty0 = smem_u32(&empty_bar[0]);
+    const uint32_t full0 = PAIR ? map_to_cta(smem_u32(&full_bar[0]), 0) : smem_u32(&full_bar[0]);
+    const uint32_t sf_col = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + SF_COL;
+    constexpr uint32_t SLOT = (1u + NSB) * ATOMS * 512u;
+    const uint32_t ring = smem_base + (uint32_t)p.stages * p.stage_bytes + (uint32_t)(TC_EPI_WARPS * p.stg_bufs) * STG_BYTES;
+    uint32_t slot = 0, phase = 0, set = 0, stage = 0, old = 0, old_phase = 0;
+    int step = 0;
     bool live = true;
     pdl_wait();
+    if (warp == SF_WARP + 4) {
+      // this one asks for them: lane 0 for A's row tile, the next for B's. Row tiles that do not exist are not copied: what their
+      // place holds meets rows and columns that are not stored.
+      for (int tile = tile0; tile < p.total_tiles && live; tile += tile_step) {
+        const Tile4 t = tile_of<PAIR>(p, tile);
+        const int rt = lane == 0 ? (t.tm * TILE_M >> 7) + (int)rank : (t.tn * p.BN >> 7) + lane - 1, rts = lane == 0 ? p.rt_a : p.rt_b;
+        const bool exists = lane < 1 + NSB && rt < rts;
+        const uint32_t count = (uint32_t)__popc(__ballot_sync(0xffffffffu, exists));
+        const uint8_t* src = (lane == 0 ? p.sa : p.sb) + ((long long)(lane > 0 && p.b_shared ? 0 : t.bz) * rts + rt) * p.kt * 512;
+        for (int kb = 0; kb < p.kblocks; ++kb, src += ATOMS * 512) {
+          const uint32_t bytes = (uint32_t)min(ATOMS, p.kt - kb * ATOMS) * 512u;
+          int ok = 1;
+          if (lane == 0) {
+            ok = mbar_wait(slot_empty0 + 8u * slot, phase ^ 1u, &abort_flag, p.status, p.wait_ns) ? 1 : 0;
+            if (ok) mbar_expect_tx(land0 + 8u * slot, count * bytes);
+          }
+          if (!__shfl_sync(0xffffffffu, ok, 0)) { live = false; break; }
+          if (exists)
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                         ::"r"(ring + slot * SLOT + (uint32_t)lane * (ATOMS * 512u)), "l"(src), "r"(bytes), "r"(land0 + 8u * slot) : "memory");
+          __syncwarp();
+          if (++slot == SF_RING) { slot = 0; phase ^= 1u; }
+        }
+      }
+      live = false;
+    }
     for (int tile = tile0; tile < p.total_tiles && live; tile += tile_step) {
       for (int kb = 0; kb < p.kblocks; ++kb) {
-        const bool ok = mbar_wait(land0 + 8u * stage, phase, &abort_flag, p.status, p.wait_ns) &&
-                        mbar_wait(sf_empty0 + 8u * set, set_phase ^ 1u, &abort_flag, p.status, p.wait_ns);
+        // The set is free once the products of the stage that had it before are through: no more sets than stages, so that stage's
+        // barrier cannot have gone round again, and this stage's barrier counts the scales of no earlier round.
+        uint32_t landed = mbar_test(land0 + 8u * slot, phase), free_set = step < p.sets || mbar_test(empty0 + 8u * old, old_phase);
+        bool ok = landed || mbar_wait(land0 + 8u * slot, phase, &abort_flag, p.status, p.wait_ns);
+        ok = ok && (free_set || mbar_wait(empty0 + 8u * old, old_phase, &abort_flag, p.status, p.wait_ns));
+        if (step >= p.sets && ++old == (uint32_t)p.stages) { old = 0; old_phase ^= 1u; }
+        ++step;
         if (!__all_sync(0xffffffffu, ok)) { live = false; break; }
         tc_fence_after();
-        const uint32_t src = smem_base + stage * p.stage_bytes + s_off;
         uint32_t v[ATOMS * 4 * (1 + NSB)];
         // columns: A's four a tile, then B's, the row tiles of one K position side by side
 #pragma unroll
         for (int i = 0; i < ATOMS * (1 + NSB); ++i) {
           const int a = i < ATOMS ? i : (i - ATOMS) / NSB, r = i < ATOMS ? 0 : 1 + (i - ATOMS) % NSB;
           asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[4 * i]), "=r"(v[4 * i + 1]), "=r"(v[4 * i + 2]), "=r"(v[4 * i + 3])
-                       : "r"(src + (uint32_t)r * (ATOMS * 512u) + 512u * a) : "memory");
+                       : "r"(ring + slot * SLOT + 16u * lane + (uint32_t)r * (ATOMS * 512u) + 512u * a) : "memory");
         }
         const uint32_t dst = sf_col + set * SF_SET;
 #pragma unroll
@@ -275,9 +295,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) { if (PAIR) mbar_arrive_cluster(sf_full0 + 8u * set); else mbar_arrive(sf_full0 + 8u * set); }
-        if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
-        if (++set == SF_SETS) { set = 0; set_phase ^= 1u; }
+        if (lane == 0) {
+          if (PAIR) mbar_arrive_cluster(full0 + 8u * stage); else mbar_arrive(full0 + 8u * stage);
+          mbar_arrive(slot_empty0 + 8u * slot);
+        }
+        __syncwarp();
+        if (++slot == SF_RING) { slot = 0; phase ^= 1u; }
+        if (++set == (uint32_t)p.sets) set = 0;
+        if (++stage == (uint32_t)p.stages) stage = 0;
       }
     }
   } else {
@@ -631,13 +656,14 @@ cudaError_t mx4_gemm_launch(const Mx4Gemm& g, cudaStream_t st, int* status, int 
   const int nsb = p.BN <= 128 ? 1 : 2;
   p.overlap = 2 * p.BN > (int)scale_column(g.fmt) ? 2 * p.BN - (int)scale_column(g.fmt) : 0;
   const uint32_t b_rows = (uint32_t)(pair ? p.BN / 2 : p.BN);
-  p.a_bytes = 128 * KB_BYTES; p.b_bytes = b_rows * KB_BYTES; p.sf_bytes = (uint32_t)atoms * 512u;
-  p.stage_bytes = p.a_bytes + p.b_bytes + (uint32_t)(1 + nsb) * p.sf_bytes;
-  p.stg_bufs = 2;
-  const uint32_t stg = (uint32_t)(TC_EPI_WARPS * p.stg_bufs) * STG_BYTES, room = SMEM_MOST - 1024 - 1024 - stg;
+  p.a_bytes = 128 * KB_BYTES; p.b_bytes = b_rows * KB_BYTES;
+  p.stage_bytes = p.a_bytes + p.b_bytes;
+  p.stg_bufs = 1;
+  const uint32_t ring = (uint32_t)(scale_ring(g.fmt) * (1 + nsb) * atoms) * 512u, stg = (uint32_t)(TC_EPI_WARPS * p.stg_bufs) * STG_BYTES, room = SMEM_MOST - 1024 - 1024 - stg - ring;
   p.stages = (int)(room / p.stage_bytes);
   if (p.stages > MAX_ST) p.stages = MAX_ST;
-  const size_t smem = 1024 + (size_t)p.stages * p.stage_bytes + stg;
+  p.sets = p.stages < SF_SETS ? p.stages : SF_SETS;
+  const size_t smem = 1024 + (size_t)p.stages * p.stage_bytes + stg + ring;
   // kind::mxf4 / mxf4nvf4: e2m1 operands (1), both K-major; scales e8m0 (1) or e4m3 (0); M / 16 and N / 8 (added per tile)
   p.idesc = 1u << 7 | 1u << 10 | (g.fmt == MXFP4 ? 1u : 0u) << 23 | (pair ? 16u : 8u) << 24;
   p.out_f32 = g.out_dtype == F32;

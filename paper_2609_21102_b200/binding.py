@@ -1,4 +1,5 @@
-"""Thin ctypes binding of libdeflpolar.so: argument marshalling only.
+"""Thin binding of libdeflpolar.so: argument marshalling only, by ctypes, or where a call is shorter than that takes by
+the module _native (csrc/native.cpp).
 
 Every function has the name and meaning of the C entry point declared in include/defl.h. Tensors
 are torch CUDA tensors used purely as device memory; all computation happens in the library's
@@ -6,7 +7,6 @@ CUDA kernels. There is no fallback: if the shared library is missing the import 
 `lib()` fails, and without a CUDA device every compute call raises.
 """
 import ctypes
-import operator
 import os
 from typing import NamedTuple, Optional
 
@@ -44,20 +44,9 @@ class DeflOpts(ctypes.Structure):
                 ("poly_terms", ctypes.c_int), ("grad_scale", ctypes.c_void_p)]
 
 
-class DeflAdamwOpts(ctypes.Structure):
-    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
-                ("weight_decay", ctypes.c_double), ("step", ctypes.c_int64), ("step_dev", ctypes.c_void_p), ("lr_dev", ctypes.c_void_p),
-                ("grad_scale", ctypes.c_void_p), ("seed", ctypes.c_uint64), ("stochastic", ctypes.c_int)]
-
-
-class DeflMx4(ctypes.Structure):
-    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
-
-
-# the tables of defl_adamw_tensor and defl_norm_tensor entries, laid out as the C compiler does
+# a defl_adamw_tensor, laid out as the C compiler does
 _ADAMW_TENSOR = np.dtype([(n, np.uint64) for n in ("p", "g", "m", "v", "m_scale", "v_scale", "copy")] +
                          [("n", np.int64), ("p_dtype", np.int32), ("g_dtype", np.int32), ("state_bits", np.int32)], align=True)
-_NORM_TENSOR = np.dtype([("x", np.uint64), ("n", np.int64), ("dtype", np.int32)], align=True)
 
 
 class DeflInfo(ctypes.Structure):
@@ -108,20 +97,8 @@ def lib():
                                       ctypes.c_void_p, ctypes.c_longlong, ctypes.c_longlong, ctypes.c_longlong,
                                       ctypes.c_void_p, ctypes.c_longlong, ctypes.c_longlong, ctypes.c_longlong,
                                       ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_float, ctypes.c_int]
-        L.defl_adamw_step.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.POINTER(DeflAdamwOpts)]
         L.defl_grad_norm_work_bytes.restype = ctypes.c_size_t
-        L.defl_grad_norm_work_bytes.argtypes = [ctypes.c_int]
-        L.defl_grad_norm.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_float] + [ctypes.c_void_p] * 3
         L.defl_mx4_codes_bytes.restype = L.defl_mx4_scales_bytes.restype = L.defl_mx4_work_bytes.restype = ctypes.c_size_t
-        L.defl_mx4_codes_bytes.argtypes = [ctypes.c_int] * 3
-        L.defl_mx4_scales_bytes.argtypes = [ctypes.c_int] * 4
-        L.defl_mx4_work_bytes.argtypes = [ctypes.c_int]
-        L.defl_mx4_quantize.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
-                                        ctypes.c_int64, ctypes.c_int64, ctypes.c_int, ctypes.POINTER(DeflMx4), ctypes.POINTER(DeflMx4),
-                                        ctypes.c_void_p]
-        L.defl_mx4_dequantize.argtypes = [ctypes.c_void_p, ctypes.POINTER(DeflMx4)] + [ctypes.c_int] * 4 + [ctypes.c_void_p, ctypes.c_int]
-        L.defl_mx4_gemm.argtypes = [ctypes.c_void_p, ctypes.POINTER(DeflMx4), ctypes.POINTER(DeflMx4)] + [ctypes.c_int] * 6 + [
-            ctypes.c_float, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64, ctypes.c_int]
         L.defl_set_profiling.argtypes = [ctypes.c_void_p, ctypes.c_int]
         L.defl_get_stage_ms.argtypes = [ctypes.c_void_p, ctypes.POINTER(ctypes.c_float), ctypes.c_int]
         L.defl_get_stage_ms_sum.argtypes = [ctypes.c_void_p, ctypes.POINTER(ctypes.c_float), ctypes.c_int, ctypes.c_int]
@@ -136,11 +113,27 @@ def lib():
     return _lib
 
 
+_calls = None
+
+
+def _native():
+    """The module that calls the library without ctypes (raises ImportError if it has not been built)."""
+    global _calls
+    if _calls is None:
+        lib()
+        from . import _native as calls
+        _calls = calls
+    return _calls
+
+
 class DeflError(RuntimeError):
     def __init__(self, code, detail=""):
         self.code = code
         msg = lib().defl_status_string(code).decode()
         super().__init__("defl error %d: %s%s" % (code, msg, (" [" + detail + "]") if detail else ""))
+
+
+_DTYPE_CODE = {torch.bfloat16: BF16, torch.float32: F32, torch.float16: F16}
 
 
 def _dtype_code(t):
@@ -211,36 +204,10 @@ class Mx4(NamedTuple):
         return t[:, :self.rows, :(self.cols + 31) // 32 * (1 if self.fmt == "mxfp4" else 2)]
 
 
-def _mx4_shapes(b, rows, cols, fmt):
-    """Shapes of codes and scales."""
-    width = (cols + 31) // 32 * 32
-    per = 128 if fmt == "mxfp4" else 64
-    return (b, rows, width // 2), (b, (rows + 127) // 128, (width + per - 1) // per, 512)
-
-
-def _gradients(grads, sizes, device):
-    """(addresses, type codes) of a list of gradients after its checks; None entries (no gradient this step) are 0 and float32.
-    Whole-list passes: a loop over the checks takes three times as long, and lists of hundreds of small tensors are bound by it."""
-    if any(g is None for g in grads):
-        some = [i for i, g in enumerate(grads) if g is not None]
-        ptr, dt = _gradients([grads[i] for i in some], None if sizes is None else [sizes[i] for i in some], device)
-        ptrs, codes = [0] * len(grads), [F32] * len(grads)
-        for i, p, d in zip(some, ptr, dt):
-            ptrs[i], codes[i] = p, d
-        return ptrs, codes
-    T = torch.Tensor
-    if set(map(T.get_device, grads)) - {device.index} or not all(map(T.is_contiguous, grads)):
-        raise ValueError("gradients must be contiguous tensors on %s" % device)
-    if sizes is not None and list(map(T.numel, grads)) != sizes:
-        raise ValueError("a gradient has another number of elements than its parameter")
-    codes = [_GRADIENT_CODE.get(d, -1) for d in map(_dtype_of, grads)]
-    if -1 in codes:
-        raise TypeError("gradients must be float32 or bfloat16")
-    return list(map(T.data_ptr, grads)), codes
-
-
-_dtype_of = operator.attrgetter("dtype")
-_GRADIENT_CODE = {torch.float32: F32, torch.bfloat16: BF16}
+def _mx4_format(fmt):
+    if fmt not in MX4_FORMATS:
+        raise ValueError("the format is mxfp4 or nvfp4, got %r" % (fmt,))
+    return MX4_FORMATS[fmt]
 
 
 class AdamWGroup:
@@ -286,6 +253,7 @@ class AdamWGroup:
             ptr = lambda t: t.data_ptr() if t is not None else 0  # noqa: E731
             self.table[i] = (ptr(p), 0, ptr(m), ptr(v), ptr(ms) if eight else 0, ptr(vs) if eight else 0, ptr(c), n, _dtype_code(p), F32,
                              8 if eight else 32)
+        self.address, self.count = self.table.ctypes.data, count
         spans.sort()
         for a, b in zip(spans, spans[1:]):
             if b[0] < a[1]:
@@ -302,11 +270,12 @@ class Context:
         if rc != 0:
             raise DeflError(rc)
         self._h = h
+        self._handle, self._index = h.value, self.device.index or 0
 
     def close(self):
         if getattr(self, "_h", None):
             lib().defl_destroy(self._h)
-            self._h = None
+            self._h = self._handle = None
 
     def __del__(self):
         try:
@@ -536,121 +505,45 @@ class Context:
         tensor [1]; grad_scale: defl_grad_norm's result, whose factor multiplies the gradients (0: the step is left out)."""
         if group.device is not None and group.device != self.device:
             raise ValueError("the group's tensors are on %s, the context is on %s" % (group.device, self.device))
-        if len(grads) != len(group.sizes):
-            raise ValueError("%d gradients for %d parameters" % (len(grads), len(group.sizes)))
-        table = group.table
-        table["g"], table["g_dtype"] = _gradients(grads, group.sizes, self.device)
-        o = DeflAdamwOpts()
-        o.beta1, o.beta2, o.eps, o.weight_decay = betas[0], betas[1], eps, weight_decay
-        if isinstance(lr, torch.Tensor):
-            o.lr_dev = self._scalar(lr, torch.float32, 1, "lr").data_ptr()
-        else:
-            o.lr = lr
-        if isinstance(step, torch.Tensor):
-            o.step_dev = self._scalar(step, torch.int64, 1, "step").data_ptr()
-        else:
-            o.step = step
-        if grad_scale is not None:
-            o.grad_scale = self._scalar(grad_scale, torch.float32, 2, "grad_scale").data_ptr() + 4
-        o.seed = seed
-        o.stochastic = int(bool(stochastic))
-        self._sync_stream()
-        self._check(lib().defl_adamw_step(self._h, table.ctypes.data, len(grads), ctypes.byref(o)))
+        self._check(_native().adamw_step(self._handle, self._index, group.address, group.count, grads, lr, step, betas[0], betas[1], eps,
+                                         weight_decay, grad_scale, stochastic, seed))
 
     def _scalar(self, t, dtype, count, what):
         if t.device != self.device or t.dtype != dtype or t.numel() != count or not t.is_contiguous():
             raise ValueError("%s must be a contiguous %s tensor of %d on %s" % (what, dtype, count, self.device))
         return t
 
+    def _result(self, r):
+        """A native call's result, or its error code raised."""
+        if type(r) is int:
+            self._check(r)
+        return r
+
     def defl_grad_norm(self, grads, max_norm=0.0, out=None, step=None):
         """out[0] = the global norm of a list of gradients (None entries are skipped), out[1] = min(1, max_norm / (norm + 1e-6)),
         or 0 if the norm is not finite; step, an int64 CUDA tensor [1], is advanced by one if it is finite. Nothing waits."""
-        out = torch.empty(2, dtype=torch.float32, device=self.device) if out is None else self._scalar(out, torch.float32, 2, "out")
-        grads = [g for g in grads if g is not None]
-        table = np.zeros(len(grads), dtype=_NORM_TENSOR)
-        if grads:
-            table["x"], table["dtype"] = _gradients(grads, None, self.device)
-            table["n"] = list(map(torch.Tensor.numel, grads))
-        if step is not None:
-            self._scalar(step, torch.int64, 1, "step")
-        work = torch.empty(int(lib().defl_grad_norm_work_bytes(len(grads))), dtype=torch.uint8, device=self.device)
-        self._sync_stream()
-        self._check(lib().defl_grad_norm(self._h, table.ctypes.data, len(grads), max_norm, out.data_ptr(),
-                                         step.data_ptr() if step is not None else None, work.data_ptr()))
-        return out
-
-    def _mx4_new(self, b, rows, cols, fmt):
-        codes, scales = _mx4_shapes(b, rows, cols, fmt)
-        return Mx4(torch.empty(codes, dtype=torch.uint8, device=self.device), torch.empty(scales, dtype=torch.uint8, device=self.device),
-                   torch.empty(b, dtype=torch.float32, device=self.device) if fmt == "nvfp4" else None, fmt, rows, cols)
-
-    def _mx4_ref(self, q, what):
-        if q.fmt not in MX4_FORMATS:
-            raise ValueError("%s: the format is mxfp4 or nvfp4, got %r" % (what, q.fmt))
-        codes, scales = _mx4_shapes(q.codes.shape[0], q.rows, q.cols, q.fmt)
-        for t, shape in ((q.codes, codes), (q.scales, scales)):
-            if t.device != self.device or t.dtype != torch.uint8 or tuple(t.shape) != shape or not t.is_contiguous():
-                raise ValueError("%s must hold contiguous uint8 tensors of shapes %s and %s on %s" % (what, codes, scales, self.device))
-        r = DeflMx4(q.codes.data_ptr(), q.scales.data_ptr(), None)
-        if q.fmt == "nvfp4":
-            if q.scale is None:
-                raise ValueError("%s needs its matrices' scales" % what)
-            r.scale = self._scalar(q.scale, torch.float32, codes[0], what + ".scale").data_ptr()
-        return r
+        return self._result(_native().grad_norm(self._handle, self._index, grads, max_norm, out, step))
 
     def defl_mx4_quantize(self, X, fmt="mxfp4", transposed=False, both=False):
         """X [b, rows, cols] (bfloat16 or float32; one of the last two strides is 1) to 4 bits: blocks along cols, an Mx4 of [rows, cols];
         `transposed`: blocks along rows, an Mx4 of the transpose [cols, rows]; `both`: a pair of them from one read."""
-        if fmt not in MX4_FORMATS:
-            raise ValueError("the format is mxfp4 or nvfp4, got %r" % (fmt,))
-        if X.ndim != 3 or X.device != self.device or X.dtype not in (torch.bfloat16, torch.float32):
-            raise ValueError("X must be a bfloat16 or float32 tensor [b, rows, cols] on %s" % self.device)
-        b, rows, cols = X.shape
-        want = (both or not transposed, both or transposed)
-        made = tuple(self._mx4_new(b, *((rows, cols) if i == 0 else (cols, rows)), fmt) if want[i] else None for i in (0, 1))
-        batch, sr, sc = X.stride()
-        order = made
-        if cols > 1 and sc != 1:
-            if rows > 1 and sr != 1:
-                raise ValueError("one of X's last two dimensions must be contiguous")
-            rows, cols, sr, order = cols, rows, sc, (made[1], made[0])     # the same matrices, seen from the other side
-        if rows == 1:
-            sr = cols
-        if sr < cols or batch < 0:
-            raise ValueError("X's rows overlap or run backwards")
-        refs = [ctypes.byref(self._mx4_ref(q, "result")) if q is not None else None for q in order]
-        work = None
-        if fmt == "nvfp4" and rows * cols > 32768:
-            work = torch.empty(int(lib().defl_mx4_work_bytes(b)), dtype=torch.uint8, device=self.device)
-        self._sync_stream()
-        self._check(lib().defl_mx4_quantize(self._h, X.data_ptr(), _dtype_code(X), b, rows, cols, sr, batch, MX4_FORMATS[fmt], refs[0],
-                                            refs[1], work.data_ptr() if work is not None else None))
-        return made if both else made[1] if transposed else made[0]
+        r = self._result(_native().mx4_quantize(self._handle, self._index, X, _mx4_format(fmt), 3 if both else 2 if transposed else 1))
+        _, rows, cols = X.shape
+        if both:
+            return Mx4(*r[0], fmt, rows, cols), Mx4(*r[1], fmt, cols, rows)
+        return Mx4(*r[1], fmt, cols, rows) if transposed else Mx4(*r[0], fmt, rows, cols)
 
     def defl_mx4_dequantize(self, q, dtype=torch.bfloat16):
-        """The values [b, rows, cols] that an Mx4 stands for."""
-        ref = self._mx4_ref(q, "q")
-        out = torch.empty((q.codes.shape[0], q.rows, q.cols), dtype=dtype, device=self.device)
-        self._sync_stream()
-        self._check(lib().defl_mx4_dequantize(self._h, ctypes.byref(ref), q.codes.shape[0], q.rows, q.cols, MX4_FORMATS[q.fmt], out.data_ptr(),
-                                              _dtype_code(out)))
-        return out
+        """The values [b, rows, cols] that an Mx4 stands for, in bfloat16 or float32."""
+        return self._result(_native().mx4_dequantize(self._handle, self._index, q.codes, q.scales, q.scale, _mx4_format(q.fmt), q.rows, q.cols,
+                                                     _DTYPE_CODE[dtype]))
 
     def defl_mx4_gemm(self, A, B, out_dtype=torch.bfloat16, out=None, alpha=1.0):
-        """alpha A B^T [b, M, N] of two Mx4 of one format that agree in cols; a B of batch 1 serves every A."""
-        ra, rb = self._mx4_ref(A, "A"), self._mx4_ref(B, "B")
-        b = A.codes.shape[0]
-        if A.fmt != B.fmt or A.cols != B.cols or B.codes.shape[0] not in (1, b):
+        """alpha A B^T [b, M, N] of two Mx4 of one format that agree in cols, in bfloat16 or float32; a B of batch 1 serves every A."""
+        if A.fmt != B.fmt or A.cols != B.cols:
             raise ValueError("A and B must agree in format, columns and batch")
-        if out is None:
-            out = torch.empty((b, A.rows, B.rows), dtype=out_dtype, device=self.device)
-        elif out.device != self.device or tuple(out.shape) != (b, A.rows, B.rows) or (B.rows > 1 and out.stride(2) != 1):
-            raise ValueError("out must be [b, M, N] on %s with contiguous rows" % self.device)
-        ld = out.stride(1) if A.rows > 1 else B.rows
-        self._sync_stream()
-        self._check(lib().defl_mx4_gemm(self._h, ctypes.byref(ra), ctypes.byref(rb), b, A.rows, B.rows, A.cols, int(B.codes.shape[0] == 1),
-                                        MX4_FORMATS[A.fmt], alpha, out.data_ptr(), ld, out.stride(0), _dtype_code(out)))
-        return out
+        return self._result(_native().mx4_gemm(self._handle, self._index, A.codes, A.scales, A.scale, B.codes, B.scales, B.scale,
+                                               _mx4_format(A.fmt), A.rows, B.rows, A.cols, out, _DTYPE_CODE[out_dtype], alpha))
 
     def defl_fill_gaussian(self, dst, seed):
         _dev(dst, "dst")

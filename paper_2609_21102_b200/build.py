@@ -6,6 +6,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdeflpolar.so")
+NATIVE = os.path.join(HERE, "_native.so")
 SOURCES = ["api.cu", "psd.cu", "gemm_simt.cu", "gemm_tc.cu", "panel.cu", "optim.cu", "mx4.cu", "mx4_gemm.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "--use_fast_math=false"]
@@ -47,7 +48,26 @@ def build(force=False, verbose=False):
     if force or procs or _stale(LIB, objs):
         cmd = [nvcc, "-shared", "-o", LIB] + objs + ["-gencode", "arch=compute_100a,code=sm_100a", "-lcudart"]
         subprocess.run(cmd, check=True)
+    build_native(force)
     return LIB
+
+
+def build_native(force=False):
+    """The Python module that calls the library without ctypes (csrc/native.cpp), against the installed torch's headers."""
+    src = os.path.join(CSRC, "native.cpp")
+    if not (force or _stale(NATIVE, [src, os.path.join(os.path.dirname(HERE), "include", "defl.h")])):
+        return NATIVE
+    import sysconfig
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-w", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+           "-I" + os.path.join(root, "include"), "-I" + os.path.join(root, "include", "torch", "csrc", "api", "include"),
+           "-I" + sysconfig.get_paths()["include"], "-I/usr/local/cuda/include", src, "-o", NATIVE,
+           # torch's libraries are in the process already; the library is found beside the module
+           "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda",
+           "-L" + HERE, "-l:libdeflpolar.so", "-Wl,-rpath,$ORIGIN"]
+    subprocess.run(cmd, check=True)
+    return NATIVE
 
 
 if __name__ == "__main__":

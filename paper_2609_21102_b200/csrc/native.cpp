@@ -1,0 +1,251 @@
+// Python module _native: argument checks, allocation of results and the calls of the operators whose kernels are shorter than
+// what ctypes and Python checks take (an AdamW step over 386 tensors 139 us, of which the library 10; a single token's
+// quantisation 22 us, its kernel 6). It calls the C interface of include/defl.h and computes nothing; binding.py documents the arguments.
+#include <Python.h>
+#include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/python_variable.h>
+#include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAStream.h>
+#include "../../include/defl.h"
+
+namespace {
+
+using at::ScalarType;
+using at::Tensor;
+
+defl_ctx* handle(PyObject* o) { return reinterpret_cast<defl_ctx*>(PyLong_AsVoidPtr(o)); }
+bool is_none(PyObject* o) { return o == Py_None; }
+const Tensor& tensor(PyObject* o, const char* what) {
+  TORCH_CHECK_TYPE(THPVariable_Check(o), what, " must be a tensor");
+  return THPVariable_Unpack(o);
+}
+void on_device(const Tensor& t, int device, const char* what) {
+  TORCH_CHECK_VALUE(t.is_cuda() && t.get_device() == device, what, " must be on cuda:", device);
+}
+// a contiguous tensor of `count` elements of one type
+void* scalar(PyObject* o, int device, ScalarType type, int64_t count, const char* what) {
+  const Tensor& t = tensor(o, what);
+  on_device(t, device, what);
+  TORCH_CHECK_VALUE(t.scalar_type() == type && t.numel() == count && t.is_contiguous(), what, " must be a contiguous ", type, " tensor of ", count, " on cuda:", device);
+  return t.data_ptr();
+}
+int code_of(ScalarType t) { return t == at::kFloat ? DEFL_F32 : t == at::kBFloat16 ? DEFL_BF16 : t == at::kHalf ? DEFL_F16 : -1; }
+Tensor make(at::IntArrayRef shape, ScalarType type, int device) {
+  return at::detail::empty_cuda(shape, type, c10::Device(c10::kCUDA, (c10::DeviceIndex)device), std::nullopt);
+}
+void use_stream(defl_ctx* c, int device) { defl_set_stream(c, c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream()); }
+
+struct Sequence {
+  PyObject* fast;
+  explicit Sequence(PyObject* o) : fast(PySequence_Fast(o, "gradients must be a list or a tuple")) { if (!fast) throw python_error(); }
+  ~Sequence() { Py_DECREF(fast); }
+  Py_ssize_t size() const { return PySequence_Fast_GET_SIZE(fast); }
+  PyObject* operator[](Py_ssize_t i) const { return PySequence_Fast_GET_ITEM(fast, i); }
+};
+// address and type of gradient i after its checks; false for None
+bool gradient(PyObject* o, Py_ssize_t i, int device, const void** x, int64_t* n, int* type) {
+  if (is_none(o)) return false;
+  TORCH_CHECK_TYPE(THPVariable_Check(o), "gradient ", i, " must be a tensor");
+  const Tensor& t = THPVariable_Unpack(o);
+  TORCH_CHECK_VALUE(t.is_cuda() && t.get_device() == device && t.is_contiguous(), "gradient ", i, " must be a contiguous tensor on cuda:", device);
+  *type = code_of(t.scalar_type());
+  TORCH_CHECK_TYPE(*type == DEFL_F32 || *type == DEFL_BF16, "gradient ", i, " must be float32 or bfloat16");
+  *x = t.data_ptr();
+  *n = t.numel();
+  return true;
+}
+
+// adamw_step(handle, device, table address, count, grads, lr, step, beta1, beta2, eps, weight_decay, grad_scale, stochastic, seed) -> code
+PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK(nargs == 14, "adamw_step takes 14 arguments");
+  defl_ctx* c = handle(a[0]);
+  const int device = (int)PyLong_AsLong(a[1]);
+  defl_adamw_tensor* table = reinterpret_cast<defl_adamw_tensor*>(PyLong_AsVoidPtr(a[2]));
+  const long count = PyLong_AsLong(a[3]);
+  const Sequence grads(a[4]);
+  TORCH_CHECK_VALUE(grads.size() == count, grads.size(), " gradients for ", count, " parameters");
+  defl_adamw_opts o = {};
+  if (THPVariable_Check(a[5])) o.lr_dev = (const float*)scalar(a[5], device, at::kFloat, 1, "lr"); else o.lr = PyFloat_AsDouble(a[5]);
+  if (THPVariable_Check(a[6])) o.step_dev = (const int64_t*)scalar(a[6], device, at::kLong, 1, "step"); else o.step = PyLong_AsLongLong(a[6]);
+  o.beta1 = PyFloat_AsDouble(a[7]); o.beta2 = PyFloat_AsDouble(a[8]); o.eps = PyFloat_AsDouble(a[9]); o.weight_decay = PyFloat_AsDouble(a[10]);
+  if (!is_none(a[11])) o.grad_scale = (const float*)scalar(a[11], device, at::kFloat, 2, "grad_scale") + 1;
+  o.stochastic = PyObject_IsTrue(a[12]);
+  o.seed = PyLong_AsUnsignedLongLongMask(a[13]);
+  if (PyErr_Occurred()) throw python_error();
+  for (long i = 0; i < count; ++i) {
+    int64_t n = 0;
+    table[i].g = nullptr;
+    if (!gradient(grads[i], i, device, &table[i].g, &n, &table[i].g_dtype)) continue;
+    TORCH_CHECK_VALUE(n == table[i].n, "gradient ", i, " has ", n, " elements, its parameter ", table[i].n);
+  }
+  use_stream(c, device);
+  return PyLong_FromLong(defl_adamw_step(c, table, (int)count, &o));
+  END_HANDLE_TH_ERRORS
+}
+
+// grad_norm(handle, device, grads, max_norm, out or None, step or None) -> out, or the error code
+PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK(nargs == 6, "grad_norm takes 6 arguments");
+  defl_ctx* c = handle(a[0]);
+  const int device = (int)PyLong_AsLong(a[1]);
+  const Sequence grads(a[2]);
+  const float max_norm = (float)PyFloat_AsDouble(a[3]);
+  int64_t* step = is_none(a[5]) ? nullptr : (int64_t*)scalar(a[5], device, at::kLong, 1, "step");
+  if (PyErr_Occurred()) throw python_error();
+  std::vector<defl_norm_tensor> table((size_t)grads.size());
+  int count = 0;
+  for (Py_ssize_t i = 0; i < grads.size(); ++i) {
+    defl_norm_tensor& t = table[count];
+    if (gradient(grads[i], i, device, &t.x, &t.n, &t.dtype)) ++count;
+  }
+  Tensor out;
+  if (is_none(a[4])) out = make({2}, at::kFloat, device); else { scalar(a[4], device, at::kFloat, 2, "out"); out = THPVariable_Unpack(a[4]); }
+  const Tensor work = make({(int64_t)defl_grad_norm_work_bytes(count)}, at::kByte, device);
+  use_stream(c, device);
+  const int rc = defl_grad_norm(c, table.data(), count, max_norm, out.data_ptr<float>(), step, work.data_ptr());
+  return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(out);
+  END_HANDLE_TH_ERRORS
+}
+
+struct Shape { int64_t codes[3], scales[4]; };
+Shape shape_of(int64_t b, int64_t rows, int64_t cols, int fmt) {
+  const int64_t width = (cols + 31) / 32 * 32, per = fmt == DEFL_MXFP4 ? 128 : 64;
+  return {{b, rows, width / 2}, {b, (rows + 127) / 128, (width + per - 1) / per, 512}};
+}
+int side(int64_t x) { return (int)(x > DEFL_MX4_MAX_SIDE ? DEFL_MX4_MAX_SIDE + 1 : x); }
+
+struct Made {
+  Tensor codes, scales, scale;
+  defl_mx4 ref;
+  Made(int64_t b, int64_t rows, int64_t cols, int fmt, int device) {
+    const Shape s = shape_of(b, rows, cols, fmt);
+    codes = make(s.codes, at::kByte, device);
+    scales = make(s.scales, at::kByte, device);
+    if (fmt == DEFL_NVFP4) scale = make({b}, at::kFloat, device);
+    ref = {codes.data_ptr(), scales.data_ptr(), scale.defined() ? scale.data_ptr<float>() : nullptr};
+  }
+  PyObject* tuple() const {
+    PyObject* s = scale.defined() ? THPVariable_Wrap(scale) : Py_NewRef(Py_None);
+    return Py_BuildValue("(NNN)", THPVariable_Wrap(codes), THPVariable_Wrap(scales), s);
+  }
+};
+
+// mx4_quantize(handle, device, X, format, which: 1 blocks along cols, 2 along rows, 3 both) -> (tuple or None, tuple or None), or the error code
+PyObject* mx4_quantize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK(nargs == 5, "mx4_quantize takes 5 arguments");
+  defl_ctx* c = handle(a[0]);
+  const int device = (int)PyLong_AsLong(a[1]), fmt = (int)PyLong_AsLong(a[3]), which = (int)PyLong_AsLong(a[4]);
+  const Tensor& X = tensor(a[2], "X");
+  TORCH_CHECK_VALUE(X.dim() == 3 && X.is_cuda() && X.get_device() == device && (X.scalar_type() == at::kBFloat16 || X.scalar_type() == at::kFloat),
+                    "X must be a bfloat16 or float32 tensor [b, rows, cols] on cuda:", device);
+  int64_t b = X.size(0), rows = X.size(1), cols = X.size(2), sr = X.stride(1), sc = X.stride(2);
+  if (b <= 0 || rows <= 0 || cols <= 0) return PyLong_FromLong(DEFL_ERR_ARG);
+  if (b > 65535 || rows > DEFL_MX4_MAX_SIDE || cols > DEFL_MX4_MAX_SIDE) return PyLong_FromLong(DEFL_ERR_RANK);
+  std::optional<Made> by_rows, by_cols;
+  if (which & 1) by_rows.emplace(b, rows, cols, fmt, device);
+  if (which & 2) by_cols.emplace(b, cols, rows, fmt, device);
+  defl_mx4* r = by_rows ? &by_rows->ref : nullptr;
+  defl_mx4* t = by_cols ? &by_cols->ref : nullptr;
+  if (cols > 1 && sc != 1) {
+    // the same matrices, seen from the other side
+    TORCH_CHECK_VALUE(rows == 1 || sr == 1, "one of X's last two dimensions must be contiguous");
+    std::swap(rows, cols);
+    std::swap(r, t);
+    sr = sc;
+  }
+  if (rows == 1) sr = cols;
+  TORCH_CHECK_VALUE(sr >= cols, "X's rows overlap");
+  Tensor work;
+  if (fmt == DEFL_NVFP4 && rows * cols > 32768) work = make({(int64_t)defl_mx4_work_bytes((int)b)}, at::kByte, device);
+  use_stream(c, device);
+  const int rc = defl_mx4_quantize(c, X.data_ptr(), code_of(X.scalar_type()), (int)b, (int)rows, (int)cols, sr, X.stride(0), fmt, r, t,
+                                   work.defined() ? work.data_ptr() : nullptr);
+  if (rc) return PyLong_FromLong(rc);
+  return Py_BuildValue("(NN)", by_rows ? by_rows->tuple() : Py_NewRef(Py_None), by_cols ? by_cols->tuple() : Py_NewRef(Py_None));
+  END_HANDLE_TH_ERRORS
+}
+
+// an Mx4's tensors (codes, scales, scale) after their checks
+defl_mx4 reference(PyObject* const* a, int fmt, int64_t rows, int64_t cols, int device, int64_t* batch, const char* what) {
+  const Tensor &codes = tensor(a[0], what), &scales = tensor(a[1], what);
+  TORCH_CHECK_VALUE(codes.dim() == 3 && scales.dim() == 4 && rows > 0 && cols > 0, what, " is not an Mx4 of its rows and columns");
+  const Shape s = shape_of(codes.size(0), rows, cols, fmt);
+  auto fine = [&](const Tensor& t, at::IntArrayRef shape) {
+    return t.is_cuda() && t.get_device() == device && t.scalar_type() == at::kByte && t.sizes() == shape && t.is_contiguous();
+  };
+  TORCH_CHECK_VALUE(fine(codes, s.codes) && fine(scales, s.scales), what, " must hold contiguous uint8 tensors of shapes ", at::IntArrayRef(s.codes), " and ",
+                    at::IntArrayRef(s.scales), " on cuda:", device);
+  *batch = codes.size(0);
+  defl_mx4 r = {codes.data_ptr(), scales.data_ptr(), nullptr};
+  if (fmt == DEFL_NVFP4) {
+    TORCH_CHECK_VALUE(!is_none(a[2]), what, " needs its matrices' scales");
+    r.scale = (float*)scalar(a[2], device, at::kFloat, *batch, what);
+  }
+  return r;
+}
+
+// mx4_dequantize(handle, device, codes, scales, scale, format, rows, cols, type code) -> tensor, or the error code
+PyObject* mx4_dequantize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK(nargs == 9, "mx4_dequantize takes 9 arguments");
+  defl_ctx* c = handle(a[0]);
+  const int device = (int)PyLong_AsLong(a[1]), fmt = (int)PyLong_AsLong(a[5]), type = (int)PyLong_AsLong(a[8]);
+  const int64_t rows = PyLong_AsLongLong(a[6]), cols = PyLong_AsLongLong(a[7]);
+  int64_t b = 0;
+  if (PyErr_Occurred()) throw python_error();
+  const defl_mx4 q = reference(a + 2, fmt, rows, cols, device, &b, "q");
+  if (b > INT_MAX || (type != DEFL_BF16 && type != DEFL_F32)) return PyLong_FromLong(DEFL_ERR_ARG);
+  Tensor out = make({b, rows, cols}, type == DEFL_BF16 ? at::kBFloat16 : at::kFloat, device);
+  use_stream(c, device);
+  const int rc = defl_mx4_dequantize(c, &q, (int)b, side(rows), side(cols), fmt, out.data_ptr(), type);
+  return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(out);
+  END_HANDLE_TH_ERRORS
+}
+
+// mx4_gemm(handle, device, A: codes, scales, scale, B: the same, format, M, N, K, out or None, type code, alpha) -> out, or the error code
+PyObject* mx4_gemm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK(nargs == 15, "mx4_gemm takes 15 arguments");
+  defl_ctx* c = handle(a[0]);
+  const int device = (int)PyLong_AsLong(a[1]), fmt = (int)PyLong_AsLong(a[8]);
+  int type = (int)PyLong_AsLong(a[13]);
+  const int64_t M = PyLong_AsLongLong(a[9]), N = PyLong_AsLongLong(a[10]), K = PyLong_AsLongLong(a[11]);
+  const double alpha = PyFloat_AsDouble(a[14]);
+  if (PyErr_Occurred()) throw python_error();
+  int64_t b = 0, bb = 0;
+  const defl_mx4 A = reference(a + 2, fmt, M, K, device, &b, "A"), B = reference(a + 5, fmt, N, K, device, &bb, "B");
+  TORCH_CHECK_VALUE(bb == 1 || bb == b, "A and B must agree in format, columns and batch");
+  Tensor out;
+  int64_t ld = N;
+  if (is_none(a[12])) {
+    if (type != DEFL_BF16 && type != DEFL_F32) return PyLong_FromLong(DEFL_ERR_ARG);
+    out = make({b, M, N}, type == DEFL_BF16 ? at::kBFloat16 : at::kFloat, device);
+  } else {
+    out = tensor(a[12], "out");
+    const int64_t want[3] = {b, M, N};
+    TORCH_CHECK_VALUE(out.is_cuda() && out.get_device() == device && out.sizes() == at::IntArrayRef(want) && (N == 1 || out.stride(2) == 1),
+                      "out must be [b, M, N] on cuda:", device, " with contiguous rows");
+    type = code_of(out.scalar_type());
+    if (M > 1) ld = out.stride(1);
+  }
+  if (b > 65535) return PyLong_FromLong(DEFL_ERR_RANK);
+  use_stream(c, device);
+  const int rc = defl_mx4_gemm(c, &A, &B, (int)b, side(M), side(N), side(K), bb == 1, fmt, (float)alpha, out.data_ptr(), ld, out.stride(0), type);
+  return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(out);
+  END_HANDLE_TH_ERRORS
+}
+
+PyMethodDef methods[] = {{"adamw_step", (PyCFunction)(void (*)(void))adamw_step, METH_FASTCALL, nullptr},
+                         {"grad_norm", (PyCFunction)(void (*)(void))grad_norm, METH_FASTCALL, nullptr},
+                         {"mx4_quantize", (PyCFunction)(void (*)(void))mx4_quantize, METH_FASTCALL, nullptr},
+                         {"mx4_dequantize", (PyCFunction)(void (*)(void))mx4_dequantize, METH_FASTCALL, nullptr},
+                         {"mx4_gemm", (PyCFunction)(void (*)(void))mx4_gemm, METH_FASTCALL, nullptr},
+                         {nullptr, nullptr, 0, nullptr}};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__native(void) { return PyModule_Create(&module); }

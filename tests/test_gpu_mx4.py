@@ -320,19 +320,22 @@ def test_refusals(ctx):
 
 
 def test_refusals_and_sizes_without_a_device():
+    import ctypes
     from paper_2609_21102_b200 import binding, build
     build.build()
     L = binding.lib()
-    assert L.defl_mx4_quantize(None, None, 0, 1, 1, 1, 1, 1, 0, None, None, None) == -1
+    with pytest.raises(ValueError):
+        binding._native().mx4_quantize(0, 0, torch.zeros(1, 4, 4), 0, 1)
+    with pytest.raises(TypeError):
+        binding._native().mx4_quantize(0, 0, None, 0, 1)
+    assert L.defl_mx4_quantize(None, None, 0, 1, 1, 1, ctypes.c_int64(1), ctypes.c_int64(1), 0, None, None, None) == -1
     assert L.defl_mx4_dequantize(None, None, 1, 1, 1, 0, None, 0) == -1
-    assert L.defl_mx4_gemm(None, None, None, 1, 1, 1, 1, 0, 0, 1.0, None, 1, 1, 0) == -1
+    assert L.defl_mx4_gemm(None, None, None, 1, 1, 1, 1, 0, 0, ctypes.c_float(1.0), None, ctypes.c_int64(1), ctypes.c_int64(1), 0) == -1
     for b, rows, cols in ((1, 1, 1), (2, 129, 33), (3, 128, 64), (1, 517, 1003)):
         for fmt, code in binding.MX4_FORMATS.items():
-            codes, scales = binding._mx4_shapes(b, rows, cols, fmt)
-            assert L.defl_mx4_codes_bytes(b, rows, cols) == int(np.prod(codes)) == b * rows * -(-cols // 32) * 16
-            assert L.defl_mx4_scales_bytes(b, rows, cols, code) == int(np.prod(scales))
             # every block of a matrix has a byte in its tiles
             index, byte, _ = mx4.quantize(np.ones((rows, cols)), fmt)
-            assert mx4.tiles(byte).size * b == int(np.prod(scales)) and index.shape[1] // 2 == codes[2]
+            assert L.defl_mx4_codes_bytes(b, rows, cols) == b * index.size // 2 == b * rows * -(-cols // 32) * 16
+            assert L.defl_mx4_scales_bytes(b, rows, cols, code) == b * mx4.tiles(byte).size
     assert L.defl_mx4_codes_bytes(0, 1, 1) == 0 and L.defl_mx4_scales_bytes(1, 1, 1, 7) == 0 and L.defl_mx4_work_bytes(0) == 0
     assert L.defl_mx4_work_bytes(1) == 592 * 4 and L.defl_mx4_work_bytes(1000) == 4000

@@ -358,12 +358,19 @@ def test_refusals_without_a_device():
     with pytest.raises(ValueError):
         binding.AdamWGroup([torch.zeros(3)], [], [])
     L = binding.lib()
-    o = binding.DeflAdamwOpts()
-    assert L.defl_adamw_step(None, None, 0, ctypes.byref(o)) == -1
-    assert L.defl_grad_norm(None, None, 0, 1.0, None, None, None) == -1
+    assert L.defl_adamw_step(None, None, 0, None) == -1
+    assert L.defl_grad_norm(None, None, 0, ctypes.c_float(1.0), None, None, None) == -1
     assert L.defl_grad_norm_work_bytes(-1) == 0
     one = L.defl_grad_norm_work_bytes(1)
     assert one == L.defl_grad_norm_work_bytes(1300) == L.defl_grad_norm_work_bytes(1301) // 2
-    # the tables are laid out as the C structures are: 7 pointers, a 64-bit count, three ints and padding
-    assert binding._ADAMW_TENSOR.itemsize == 80 and binding._NORM_TENSOR.itemsize == 24
-    assert ctypes.sizeof(binding.DeflAdamwOpts) == 88
+    # the table is laid out as the C structure is: 7 pointers, a 64-bit count, three ints and padding
+    assert binding._ADAMW_TENSOR.itemsize == 80
+    # a context that is closed refuses (no device: none can be made), and so does a list that is none
+    with pytest.raises(TypeError):
+        binding._native().grad_norm(0, 0, 5, 1.0, None, None)
+    with pytest.raises(ValueError):
+        binding._native().grad_norm(0, 0, [torch.zeros(3)], 1.0, None, None)
+    with pytest.raises(TypeError):
+        binding._native().grad_norm(0, 0, [3], 1.0, None, None)
+    with pytest.raises(ValueError):
+        binding._native().adamw_step(0, 0, 0, 1, [], 1e-3, 1, 0.9, 0.999, 1e-8, 0.0, None, False, 0)

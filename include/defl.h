@@ -380,7 +380,7 @@ int defl_grad_norm(defl_ctx* ctx, const defl_norm_tensor* tensors, int count, fl
  * columns; a product contracts two such matrices along their columns, D = A B^T.
  *   DEFL_MXFP4  blocks of 32; scale 2^e (a byte e + 127), the smallest power of two with largest magnitude <= 6 * 2^e
  *   DEFL_NVFP4  blocks of 16; scale s * 2^w: w one number per matrix (held as scale = 2^w), the smallest with largest magnitude of the
- *               matrix <= 6 * 448 * 2^w; s the e4m3 number nearest (ties to even) to the fp32 quotient (largest * 2^-w) / 6. The
+ *               matrix <= 6 * 448 * 2^w, at least 2^-100; s the e4m3 number nearest (ties to even) to the fp32 quotient (largest * 2^-w) / 6. The
  *               matrix's scale is a power of two so that it costs no rounding; the products take any positive fp32 there.
  * A code is the e2m1 number nearest to value / scale, ties to even. A block that holds Inf or NaN has a NaN for its scale (byte
  * 255, or e4m3's 0x7f) and makes NaN of what it enters; the rest of the matrix is as if those values were zero.

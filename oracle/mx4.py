@@ -27,14 +27,14 @@ def nearest_even(x, grid):
 
 
 def whole_scale(X, fmt):
-    """The matrix's own scale: the smallest power of two with |X| <= 6 * 448 * 2^w, from the values that are finite."""
+    """The matrix's own scale: the smallest power of two (from 2^-100 on) with |X| <= 6 * 448 * 2^w, from the values that are finite."""
     if fmt == "mxfp4":
         return 1.0
     a = np.abs(X[np.isfinite(X)])
     top = a.max() if a.size else 0.0
     if top == 0.0:
         return 1.0
-    w = -126
+    w = -100
     while top > 2688.0 * 2.0 ** w:
         w += 1
     return 2.0 ** w

@@ -47,46 +47,69 @@ __device__ __forceinline__ uint32_t e2m1x8(const float* v) {
 }
 
 // exponent byte of the power of two of an nvfp4 matrix whose largest magnitude has these bits: the smallest with
-// largest <= 448 * 6 * 2^w (2688 = 1.3125 * 2^11), at least 2^-126; 1 for a matrix of zeros
+// largest <= 448 * 6 * 2^w (2688 = 1.3125 * 2^11), at least 2^-100 (so that a block's scale and its reciprocal stay ordinary
+// numbers); 1 for a matrix of zeros
 __device__ __forceinline__ int whole_exponent(uint32_t top) {
   if (top == 0u) return 127;
   const int e = (int)((top + 0x57ffffu) >> 23) - 11;
-  return e > 1 ? e : 1;
+  return e > 27 ? e : 27;
 }
 
-// What a block's values are multiplied by, and its scale byte.
+// A block's scale byte and what its values are multiplied by.
 struct BlockScale {
-  float pre, r, s;        // mxfp4: value * r. nvfp4: value * pre / s, r = 1 / s
+  float r, lo, s;         // mxfp4: value * r. nvfp4: the quotient value / s with r (+ lo) = 1 / s
   uint32_t byte;
 };
-template <int FMT>
-__device__ __forceinline__ BlockScale block_scale(uint32_t big, float pre) {
+// `whole` = 2^w, `unit` = 2^-w
+template <int FMT, bool SHORT>
+__device__ __forceinline__ BlockScale block_scale(uint32_t big, float whole, float unit) {
   BlockScale q;
-  q.pre = pre;
+  q.lo = q.s = 0.f;
   if (FMT == MXFP4) {
     // the smallest power of two with big <= 6 * 2^e = 1.5 * 2^(e + 2). (The usual rule 2^(floor(log2 big) - 2) clips whatever
     // lies above 6 of 8, up to a quarter of the block's largest value.)
     const int byte = (int)((big + 0x3fffffu) >> 23) - 2;
     q.byte = byte > 0 ? (uint32_t)byte : 0u;
     q.r = __uint_as_float((254u - q.byte) << 23);
-    q.s = 0.f;
     if (big >= 0x7f800000u) q.byte = 255u;                    // NaN: Inf and NaN have no place in a block
   } else {
-    const float a = __fdiv_rn(__uint_as_float(big) * pre, 6.f);
+    // big * 2^-w / 6 correctly rounded: the product with the rounded reciprocal, and one correction by its exact remainder
+    // (Markstein 1990)
+    const float x = __uint_as_float(big) * unit, sixth = 1.f / 6.f, t = x * sixth, a = fmaf(fmaf(-t, 6.f, x), sixth, t);
     q.byte = (uint32_t)__nv_cvt_float_to_fp8(a, __NV_SATFINITE, __NV_E4M3);
-    q.s = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)q.byte, __NV_E4M3)));
-    q.r = q.s > 0.f ? __frcp_rn(q.s) : 0.f;
+    q.s = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)q.byte, __NV_E4M3))) * whole;
+    const float r = q.s > 0.f ? __frcp_rn(q.s) : 0.f;
+    if (SHORT) {
+      // r in two parts, the first of 16 bits
+      q.r = __uint_as_float(__float_as_uint(r) & 0xffffff00u);
+      q.lo = q.s > 0.f ? fmaf(-q.r, q.s, 1.f) * r : 0.f;
+    } else {
+      q.r = r;
+    }
     if (big >= 0x7f800000u) q.byte = 0x7fu;
   }
   return q;
 }
-// The quotient x * pre / s correctly rounded: the product with the rounded reciprocal, and one correction by its exact
-// remainder (Markstein 1990). The plain product would miss the ties between two codes, which values of few bits often hit.
-template <int FMT>
+// The quotient value / s correctly rounded, so that the ties between two codes, which values of few bits often hit, are ties.
+// SHORT (values of 8 bits): value * r.hi is exact and value * r.lo brings the sum to 2^-39 of the quotient, far nearer than any
+// quotient that is not a tie comes to one. Else the rounded product and one correction by its exact remainder (Markstein 1990).
+template <int FMT, bool SHORT>
 __device__ __forceinline__ float scaled(float x, const BlockScale& q) {
   if (FMT == MXFP4) return x * q.r;
-  const float y = x * q.pre, a = y * q.r;
-  return fmaf(fmaf(-a, q.s, y), q.r, a);
+  if (SHORT) return fmaf(x, q.lo, x * q.r);
+  const float a = x * q.r;
+  return fmaf(fmaf(-a, q.s, x), q.r, a);
+}
+
+// the larger magnitudes of two pairs of bf16 (signs mean nothing), NaN above all
+__device__ __forceinline__ uint32_t max_magnitudes(uint32_t a, uint32_t b) {
+  asm("max.NaN.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
+  return a;
+}
+// the two bf16 of a word times a power of two, in fp32
+__device__ __forceinline__ void widen(uint32_t w, uint16_t power, float& lo, float& hi) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tfma.rn.f32.bf16 %0, l, %3, 0f00000000;\n\tfma.rn.f32.bf16 %1, h, %3, 0f00000000;\n\t}"
+      : "=f"(lo), "=f"(hi) : "r"(w), "h"(power));
 }
 
 // Where a row of the tile starts in shared memory, in words: rows of 32 columns further on are shifted by 8 words, so that the
@@ -119,10 +142,10 @@ __global__ void __launch_bounds__(Q_THREADS) mx4_quantize_kernel(const QuantPara
     const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem);
 #pragma unroll
     for (int i = 0; i < TILE * PER / Q_THREADS; ++i) {
-      const int u = tid + Q_THREADS * i, r = u / PER, c = (u % PER) * (16 / ES);
+      const int u = tid + Q_THREADS * i, r = u / PER, c = (tid % PER) * (16 / ES);
       int left = row0 + r < p.rows ? (p.cols - col0 - c) * ES : 0;
       left = left < 0 ? 0 : left > 16 ? 16 : left;
-      copy16(base + 4 * row_word<T>(r) + (u % PER) * 16, left ? X + (long long)(row0 + r) * p.ld + col0 + c : X, (uint32_t)left);
+      copy16(base + 4 * row_word<T>(r) + (tid % PER) * 16, left ? X + (long long)(row0 + r) * p.ld + col0 + c : X, (uint32_t)left);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   } else {
@@ -134,7 +157,7 @@ __global__ void __launch_bounds__(Q_THREADS) mx4_quantize_kernel(const QuantPara
       reinterpret_cast<T*>(words + row_word<T>(r))[c] = x;
     }
   }
-  float pre = 1.f;
+  float whole = 1.f, unit = 1.f;
   if (FMT == NVFP4) {
     uint32_t top = 0;
     if (p.nper > 0) {
@@ -154,54 +177,92 @@ __global__ void __launch_bounds__(Q_THREADS) mx4_quantize_kernel(const QuantPara
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < Q_THREADS / 32; ++i) top = max(top, s_top[i]);
-    const int e = whole_exponent(top);
-    pre = __uint_as_float((uint32_t)(254 - e) << 23);
+    const uint32_t e = (uint32_t)whole_exponent(top);
+    whole = __uint_as_float(e << 23);
+    unit = __uint_as_float((254u - e) << 23);
     if (blockIdx.x == 0 && tid == 0) {
-      const float whole = __uint_as_float((uint32_t)e << 23);
       if (p.rscale) p.rscale[bz] = whole;
       if (p.cscale) p.cscale[bz] = whole;
     }
   }
 
   if (p.rc) {
-    const int width = mx4_width(p.cols);
+    // A lane takes 32 values of a row, in four pieces of eight codes. Its first piece is number `rot`, so that the eight lanes of a
+    // shared-memory access meet all banks (fp32: and the second half of a piece first in every other lane).
+    const int width = mx4_width(p.cols), rot = (lane >> 1) & 3, odd = lane & 1;
     uint8_t* const out = p.rc + (long long)bz * p.rows * (width / 2);
-#pragma unroll 4
-    for (int i = 0; i < TILE * TILE / 8 / Q_THREADS; ++i) {
-      const int u = tid + Q_THREADS * i, r = u >> 4, c8 = u & 15;
-      float v[8];
-      uint32_t big = 0;
-      if (ES == 2) {
-        const uint4 q = *reinterpret_cast<const uint4*>(words + row_word<T>(r) + 4 * c8);
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll 1
+    for (int i = 0; i < TILE * TILE / 32 / Q_THREADS; ++i) {
+      const int u = tid + Q_THREADS * i, r = u >> 2, g = u & 3;
+      const uint32_t* const src = words + row_word<T>(r) + g * (8 * ES);
+      uint32_t w[8 * ES], big[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          big = __vmaxu2(big, w[j] & 0x7fff7fffu);
-          v[2 * j] = __uint_as_float(w[j] << 16);
-          v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+      for (int k = 0; k < 4; ++k) {
+        const int piece = (k + rot) & 3;
+        if (ES == 2) {
+          const uint4 q = *reinterpret_cast<const uint4*>(src + 4 * piece);
+          w[4 * k] = q.x; w[4 * k + 1] = q.y; w[4 * k + 2] = q.z; w[4 * k + 3] = q.w;
+          const uint32_t m = max_magnitudes(max_magnitudes(q.x, q.y), max_magnitudes(q.z, q.w)) & 0x7fff7fffu;
+          big[k] = max(m << 16, m & 0xffff0000u);
+        } else {
+          uint32_t m = 0;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint4 q = *reinterpret_cast<const uint4*>(src + 8 * piece + 4 * (h ^ odd));
+            w[8 * k + 4 * h] = q.x; w[8 * k + 4 * h + 1] = q.y; w[8 * k + 4 * h + 2] = q.z; w[8 * k + 4 * h + 3] = q.w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) m = max(m, w[8 * k + 4 * h + j] & 0x7fffffffu);
+          }
+          big[k] = m;
         }
-#pragma unroll
-        for (int o = 1; o < BLK / 8; o <<= 1) big = __vmaxu2(big, __shfl_xor_sync(0xffffffffu, big, o));
-        big = max(big << 16, big & 0xffff0000u);
+      }
+      // blocks of 16: which pieces are the first block's depends on the lane (the pair that starts at piece 0 or 2, or one of each)
+      BlockScale q[2];
+      if (FMT == MXFP4) {
+        q[0] = block_scale<FMT, ES == 2>(max(max(big[0], big[1]), max(big[2], big[3])), whole, unit);
+        q[1] = q[0];
       } else {
-        const float4* f = reinterpret_cast<const float4*>(words + row_word<T>(r) + 8 * c8);
-        const float4 a = f[0], b = f[1];
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) big = max(big, magnitude_bits(v[j]));
-#pragma unroll
-        for (int o = 1; o < BLK / 8; o <<= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
+        const uint32_t even = max(big[0], big[1]), mid = max(big[1], big[2]), last = max(big[2], big[3]), ends = max(big[3], big[0]);
+        const uint32_t b0 = rot == 0 ? even : rot == 1 ? ends : rot == 2 ? last : mid, b1 = rot == 0 ? last : rot == 1 ? mid : rot == 2 ? even : ends;
+        q[0] = block_scale<FMT, ES == 2>(b0, whole, unit);
+        q[1] = block_scale<FMT, ES == 2>(b1, whole, unit);
       }
-      const BlockScale q = block_scale<FMT>(big, pre);
+      uint32_t codes[4];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = scaled<FMT>(v[j], q);
-      const uint32_t codes = e2m1x8(v);
-      if (row0 + r < p.rows && col0 + 8 * c8 < width)
-        *reinterpret_cast<uint32_t*>(out + (long long)(row0 + r) * (width / 2) + (col0 + 8 * c8) / 2) = codes;
-      if (c8 % (BLK / 8) == 0) {
-        const int blk = c8 / (BLK / 8);
-        s_row[(blk >> 2) * 512 + (r & 31) * 16 + (r >> 5) * 4 + (blk & 3)] = (uint8_t)q.byte;
+      for (int k = 0; k < 4; ++k) {
+        BlockScale c = q[0];
+        if (FMT == NVFP4) {
+          const bool second = ((k + rot) & 2) != 0;
+          c.r = second ? q[1].r : q[0].r; c.lo = second ? q[1].lo : q[0].lo; c.s = second ? q[1].s : q[0].s;
+        }
+        float v[8];
+        if (ES == 2) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t x = w[4 * k + j];
+            if (FMT == MXFP4) {
+              widen(x, (uint16_t)(__float_as_uint(c.r) >> 16), v[2 * j], v[2 * j + 1]);
+            } else {
+              v[2 * j] = scaled<FMT, true>(__uint_as_float(x << 16), c);
+              v[2 * j + 1] = scaled<FMT, true>(__uint_as_float(x & 0xffff0000u), c);
+            }
+          }
+          codes[k] = e2m1x8(v);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = scaled<FMT, false>(__uint_as_float(w[8 * k + j]), c);
+          const uint32_t x = e2m1x8(v);
+          codes[k] = odd ? __byte_perm(x, x, 0x1032) : x;
+        }
       }
+      // the pieces back in their places
+      if (rot & 1) { const uint32_t x = codes[3]; codes[3] = codes[2]; codes[2] = codes[1]; codes[1] = codes[0]; codes[0] = x; }
+      if (rot & 2) { uint32_t x = codes[0]; codes[0] = codes[2]; codes[2] = x; x = codes[1]; codes[1] = codes[3]; codes[3] = x; }
+      if (row0 + r < p.rows && col0 + 32 * g < width)
+        *reinterpret_cast<uint4*>(out + (long long)(row0 + r) * (width / 2) + (col0 + 32 * g) / 2) = make_uint4(codes[0], codes[1], codes[2], codes[3]);
+      uint8_t* const sb = s_row + (r & 31) * 16 + (r >> 5) * 4;
+      if (FMT == MXFP4) sb[g] = (uint8_t)q[0].byte;
+      else *reinterpret_cast<uint16_t*>(sb + (g >> 1) * 512 + (g & 1) * 2) = (uint16_t)(q[0].byte | q[1].byte << 8);
     }
   }
 
@@ -216,26 +277,35 @@ __global__ void __launch_bounds__(Q_THREADS) mx4_quantize_kernel(const QuantPara
       uint32_t w[32];
 #pragma unroll
       for (int j = 0; j < 32; ++j) w[j] = words[row_word<T>(32 * rb) + j * (TILE * ES / 4) + cw];
+      uint32_t big[32 / BLK];
+#pragma unroll
+      for (int h = 0; h < 32 / BLK; ++h) {
+        uint32_t m = ES == 4 ? w[BLK * h] & 0x7fffffffu : w[BLK * h];
+#pragma unroll
+        for (int j = 1; j < BLK; ++j) m = ES == 4 ? max(m, w[BLK * h + j] & 0x7fffffffu) : max_magnitudes(m, w[BLK * h + j]);
+        big[h] = m;
+      }
 #pragma unroll
       for (int k = 0; k < COLS; ++k) {
         const int c = cw * COLS + k;
         uint32_t codes[4];
 #pragma unroll
         for (int h = 0; h < 32 / BLK; ++h) {
-          uint32_t big = 0;
-#pragma unroll
-          for (int j = 0; j < BLK; ++j) {
-            const uint32_t x = ES == 4 ? w[BLK * h + j] & 0x7fffffffu : (k == 0 ? w[BLK * h + j] << 16 : w[BLK * h + j]) & 0x7fff0000u;
-            big = max(big, x);
-          }
-          const BlockScale q = block_scale<FMT>(big, pre);
+          const uint32_t m = ES == 4 ? big[h] : (k == 0 ? big[h] << 16 : big[h]) & 0x7fff0000u;
+          const BlockScale q = block_scale<FMT, ES == 2>(m, whole, unit);
 #pragma unroll
           for (int o = 0; o < BLK / 8; ++o) {
             float v[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
               const uint32_t x = w[BLK * h + 8 * o + j];
-              v[j] = scaled<FMT>(__uint_as_float(ES == 4 ? x : k == 0 ? x << 16 : x & 0xffff0000u), q);
+              if (ES == 2 && FMT == MXFP4) {
+                float lo, hi;
+                widen(x, (uint16_t)(__float_as_uint(q.r) >> 16), lo, hi);
+                v[j] = k == 0 ? lo : hi;
+              } else {
+                v[j] = scaled<FMT, ES == 2>(__uint_as_float(ES == 4 ? x : k == 0 ? x << 16 : x & 0xffff0000u), q);
+              }
             }
             codes[(BLK / 8) * h + o] = e2m1x8(v);
           }
@@ -263,36 +333,61 @@ __global__ void __launch_bounds__(Q_THREADS) mx4_quantize_kernel(const QuantPara
   }
 }
 
-// Largest finite magnitude of a part of each matrix (nvfp4): rows are dealt to the CTAs of a matrix.
+// Largest finite magnitude of a part of each matrix (nvfp4): its 16-byte pieces are dealt to the CTAs of a matrix. Bound by HBM
+// (or L2): four pieces of a thread are on their way at a time. A thread that has met Inf or NaN looks again without them.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(Q_THREADS) mx4_amax_kernel(const void* Xv, long long ld, long long batch_stride, int rows, int cols, float* partial) {
   __shared__ uint32_t s_top[Q_THREADS / 32];
   pdl_wait();
   const T* const X = reinterpret_cast<const T*>(Xv) + (long long)blockIdx.y * batch_stride;
   constexpr int V = 16 / (int)sizeof(T);
-  const long long per = VEC ? (cols + V - 1) / V : cols, count = per * rows, step = (long long)gridDim.x * Q_THREADS;
   uint32_t top = 0;
-  // (row and column are carried along: the step is a fixed number of rows and columns)
-  const long long u0 = (long long)blockIdx.x * Q_THREADS + threadIdx.x;
-  long long r = u0 / per, c = u0 - r * per;
-  const long long dr = step / per, dc = step - dr * per;
-#pragma unroll 4
-  for (long long u = u0; u < count; u += step) {
-    if (VEC && c * V + V <= cols) {
-      const uint4 q = *reinterpret_cast<const uint4*>(X + r * ld + c * V);
+  for (int pass = 0; pass < 2; ++pass) {
+    top = 0;
+    const bool fine = pass == 1;
+    auto take = [&](const uint4& q) {
       const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if (sizeof(T) == 4) top = max(top, finite_or_zero(w[j] & 0x7fffffffu));
+        if (sizeof(T) == 4) top = max(top, fine ? finite_or_zero(w[j] & 0x7fffffffu) : w[j] & 0x7fffffffu);
+        else if (!fine) top = __vmaxu2(top, w[j] & 0x7fff7fffu);
         else top = max(top, max(finite_or_zero((w[j] << 16) & 0x7fff0000u), finite_or_zero(w[j] & 0x7fff0000u)));
       }
+    };
+    auto one = [&](T x) {
+      const uint32_t m = fine ? finite_or_zero(magnitude_bits(x)) : magnitude_bits(x);
+      if (sizeof(T) == 2 && !fine) top = __vmaxu2(top, m); else top = max(top, m);
+    };
+    const long long step = (long long)gridDim.x * Q_THREADS, u0 = (long long)blockIdx.x * Q_THREADS + threadIdx.x;
+    if (VEC && (ld == cols || rows == 1)) {
+      const long long n = (long long)rows * cols, nv = n / V;
+      const uint4* const P = reinterpret_cast<const uint4*>(X);
+      long long u = u0;
+      for (; u + 3 * step < nv; u += 4 * step) {
+        const uint4 a = P[u], b = P[u + step], c = P[u + 2 * step], d = P[u + 3 * step];
+        take(a); take(b); take(c); take(d);
+      }
+      for (; u < nv; u += step) take(P[u]);
+      if (u0 < n - nv * V) one(X[nv * V + u0]);
     } else {
-      const int n = VEC ? V : 1;
-      for (int j = 0; j < n; ++j)
-        if (c * n + j < cols) top = max(top, finite_or_zero(magnitude_bits(X[r * ld + c * n + j])));
+      const long long per = VEC ? (cols + V - 1) / V : cols;
+      // (row and column are carried along: the step is a fixed number of rows and columns)
+      long long r = u0 / per, c = u0 - r * per;
+      const long long dr = step / per, dc = step - dr * per;
+      for (; r < rows;) {
+        if (VEC && c * V + V <= cols) {
+          take(*reinterpret_cast<const uint4*>(X + r * ld + c * V));
+        } else {
+          const int n = VEC ? V : 1;
+          for (int j = 0; j < n; ++j)
+            if (c * n + j < cols) one(X[r * ld + c * n + j]);
+        }
+        r += dr; c += dc;
+        if (c >= per) { c -= per; ++r; }
+      }
     }
-    r += dr; c += dc;
-    if (c >= per) { c -= per; ++r; }
+    if (sizeof(T) == 2 && !fine) top = max(top << 16, top & 0xffff0000u);
+    if (top < 0x7f800000u) break;
   }
   top = __reduce_max_sync(0xffffffffu, top);
   if ((threadIdx.x & 31) == 0) s_top[threadIdx.x >> 5] = top;

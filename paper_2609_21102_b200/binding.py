@@ -204,12 +204,6 @@ class Mx4(NamedTuple):
         return t[:, :self.rows, :(self.cols + 31) // 32 * (1 if self.fmt == "mxfp4" else 2)]
 
 
-def _mx4_format(fmt):
-    if fmt not in MX4_FORMATS:
-        raise ValueError("the format is mxfp4 or nvfp4, got %r" % (fmt,))
-    return MX4_FORMATS[fmt]
-
-
 class AdamWGroup:
     """The tensors of defl_adamw_step, checked once: parameters (float32 or bfloat16), first and second moments of the same
     sizes, all float32 or, in 8 bits, float8_e4m3fn with float32 scales [ceil(n / 256)] (the second moment is held as its
@@ -527,15 +521,12 @@ class Context:
     def defl_mx4_quantize(self, X, fmt="mxfp4", transposed=False, both=False):
         """X [b, rows, cols] (bfloat16 or float32; one of the last two strides is 1) to 4 bits: blocks along cols, an Mx4 of [rows, cols];
         `transposed`: blocks along rows, an Mx4 of the transpose [cols, rows]; `both`: a pair of them from one read."""
-        r = self._result(_native().mx4_quantize(self._handle, self._index, X, _mx4_format(fmt), 3 if both else 2 if transposed else 1))
-        _, rows, cols = X.shape
-        if both:
-            return Mx4(*r[0], fmt, rows, cols), Mx4(*r[1], fmt, cols, rows)
-        return Mx4(*r[1], fmt, cols, rows) if transposed else Mx4(*r[0], fmt, rows, cols)
+        r = _native().mx4_quantize(self._handle, self._index, X, fmt, 3 if both else 2 if transposed else 1, Mx4)
+        return r if type(r) is not int else self._result(r)
 
     def defl_mx4_dequantize(self, q, dtype=torch.bfloat16):
         """The values [b, rows, cols] that an Mx4 stands for, in bfloat16 or float32."""
-        return self._result(_native().mx4_dequantize(self._handle, self._index, q.codes, q.scales, q.scale, _mx4_format(q.fmt), q.rows, q.cols,
+        return self._result(_native().mx4_dequantize(self._handle, self._index, q.codes, q.scales, q.scale, q.fmt, q.rows, q.cols,
                                                      _DTYPE_CODE[dtype]))
 
     def defl_mx4_gemm(self, A, B, out_dtype=torch.bfloat16, out=None, alpha=1.0):
@@ -543,7 +534,7 @@ class Context:
         if A.fmt != B.fmt or A.cols != B.cols:
             raise ValueError("A and B must agree in format, columns and batch")
         return self._result(_native().mx4_gemm(self._handle, self._index, A.codes, A.scales, A.scale, B.codes, B.scales, B.scale,
-                                               _mx4_format(A.fmt), A.rows, B.rows, A.cols, out, _DTYPE_CODE[out_dtype], alpha))
+                                               A.fmt, A.rows, B.rows, A.cols, out, _DTYPE_CODE[out_dtype], alpha))
 
     def defl_fill_gaussian(self, dst, seed):
         _dev(dst, "dst")

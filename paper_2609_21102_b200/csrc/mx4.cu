@@ -163,7 +163,23 @@ __global__ void __launch_bounds__(Q_THREADS) mx4_quantize_kernel(const QuantPara
     if (p.nper > 0) {
       for (int i = tid; i < p.nper; i += Q_THREADS) top = max(top, __float_as_uint(p.partial[(long long)bz * p.nper + i]));
     } else {
-      for (int u = tid; u < p.rows * p.cols; u += Q_THREADS) {
+      constexpr int V = 16 / ES;
+      int done = 0;
+      if (VEC && (p.ld == p.cols || p.rows == 1)) {
+        done = p.rows * p.cols / V * V;
+#pragma unroll 4
+        for (int u = tid; u < done / V; u += Q_THREADS) {
+          const uint4 q = reinterpret_cast<const uint4*>(X)[u];
+          const uint32_t x[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if (ES == 4) top = max(top, finite_or_zero(x[j] & 0x7fffffffu));
+            else top = max(top, max(finite_or_zero((x[j] << 16) & 0x7fff0000u), finite_or_zero(x[j] & 0x7fff0000u)));
+          }
+        }
+      }
+#pragma unroll 4
+      for (int u = done + tid; u < p.rows * p.cols; u += Q_THREADS) {
         const int r = u / p.cols;
         top = max(top, finite_or_zero(magnitude_bits(X[(long long)r * p.ld + (u - r * p.cols)])));
       }

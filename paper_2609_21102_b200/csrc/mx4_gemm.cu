@@ -431,10 +431,13 @@ struct RowParams {
   float alpha;
 };
 
-// LPR lanes a row of B: 16 where there are rows enough, else the whole CTA. T >= M rows of A.
+// LPR lanes a row of B: 16 where there are rows enough, else half the CTA. T >= M rows of A. The weights are asked for ahead of
+// everything else, a group of pieces (32 codes) a lane, and the next group before one is worked on: a call of one token is a few
+// microseconds, of which the first trip to memory is one.
 template <int FMT, int T, int LPR>
 __global__ void __launch_bounds__(ROW_THREADS) mx4_row_kernel(const RowParams p) {
-  constexpr int BLK = FMT == MXFP4 ? 32 : 16, NB = 32 / BLK;
+  constexpr int BLK = FMT == MXFP4 ? 32 : 16, NB = 32 / BLK, GROUP = LPR == 16 ? 4 : 1;
+  static_assert(ROW_CHUNK / 32 % (LPR * GROUP) == 0, "a group does not straddle two chunks");
   __shared__ __align__(16) int8_t s_a[T][ROW_CHUNK];
   __shared__ float s_sc[T][ROW_CHUNK / BLK];
   __shared__ float s_part[ROW_THREADS / 32][T];
@@ -450,15 +453,31 @@ __global__ void __launch_bounds__(ROW_THREADS) mx4_row_kernel(const RowParams p)
   const uint8_t* const ws = p.B.scales + ((long long)bb * mx4_row_tiles(p.N) + (nr >> 7)) * kt * 512 + (nr & 31) * 16 + ((nr >> 5) & 3) * 4;
   const uint8_t* const ac = p.A.codes + (long long)bz * p.M * (width / 2);
   const uint8_t* const as = p.A.scales + (long long)bz * mx4_row_tiles(p.M) * kt * 512;
+  uint4 next[GROUP];
+  uint32_t next_sb[GROUP];
+  auto fetch = [&](int first) {
+#pragma unroll
+    for (int k = 0; k < GROUP; ++k) {
+      const int i = first + at0 + k * LPR;
+      next[k] = make_uint4(0, 0, 0, 0);
+      next_sb[k] = 0;
+      if (row_ok && i < pieces) {
+        next[k] = w[i];
+        if (FMT == MXFP4) next_sb[k] = ws[(long long)(i >> 2) * 512 + (i & 3)];
+        else next_sb[k] = *reinterpret_cast<const uint16_t*>(ws + (long long)(i >> 1) * 512 + (i & 1) * 2);
+      }
+    }
+  };
   float sum[T];
 #pragma unroll
   for (int t = 0; t < T; ++t) sum[t] = 0.f;
   pdl_wait();
+  fetch(0);
   for (int k0 = 0; k0 < width; k0 += ROW_CHUNK) {
     const int kn = min(ROW_CHUNK, width - k0);
     if (k0) __syncthreads();
     for (int u = tid; u < T * (kn / 8); u += ROW_THREADS) {
-      const int t = u / (kn / 8), o = u - t * (kn / 8);
+      const int t = T == 1 ? 0 : u / (kn / 8), o = u - t * (kn / 8);
       uint32_t codes = 0;
       if (t < p.M) codes = *reinterpret_cast<const uint32_t*>(ac + (long long)t * (width / 2) + k0 / 2 + 4 * o);
       // signed bytes: the positive ones less the negative ones, byte by byte
@@ -467,21 +486,24 @@ __global__ void __launch_bounds__(ROW_THREADS) mx4_row_kernel(const RowParams p)
       *reinterpret_cast<uint2*>(&s_a[t][8 * o]) = make_uint2(lo, hi);
     }
     for (int u = tid; u < T * (kn / BLK); u += ROW_THREADS) {
-      const int t = u / (kn / BLK), j = u - t * (kn / BLK), blk = k0 / BLK + j;
+      const int t = T == 1 ? 0 : u / (kn / BLK), j = u - t * (kn / BLK), blk = k0 / BLK + j;
       float s = 0.f;
       if (t < p.M) s = 0.25f * scale_value<FMT>(as[(long long)(blk >> 2) * 512 + (t & 31) * 16 + (blk & 3)]);
       s_sc[t][j] = s;
     }
     __syncthreads();
-    if (row_ok) {
-      const int first = k0 / 32, last = min(pieces, first + ROW_CHUNK / 32);
-#pragma unroll 4
-      for (int i = first + at0; i < last; i += LPR) {
-        const uint4 q = w[i];
-        uint32_t sb;
-        if (FMT == MXFP4) sb = ws[(long long)(i >> 2) * 512 + (i & 3)];
-        else sb = *reinterpret_cast<const uint16_t*>(ws + (long long)(i >> 1) * 512 + (i & 1) * 2);
-        const uint32_t c[4] = {q.x, q.y, q.z, q.w};
+    const int first = k0 / 32, last = first + kn / 32;
+    for (int i0 = first; i0 < last; i0 += GROUP * LPR) {
+      uint4 cur[GROUP];
+      uint32_t cur_sb[GROUP];
+#pragma unroll
+      for (int k = 0; k < GROUP; ++k) { cur[k] = next[k]; cur_sb[k] = next_sb[k]; }
+      fetch(i0 + GROUP * LPR);
+#pragma unroll
+      for (int k = 0; k < GROUP; ++k) {
+        const int i = i0 + at0 + k * LPR;
+        if (i >= last) break;
+        const uint32_t c[4] = {cur[k].x, cur[k].y, cur[k].z, cur[k].w};
 #pragma unroll
         for (int t = 0; t < T; ++t) {
           const uint4* a4 = reinterpret_cast<const uint4*>(&s_a[t][(i - first) * 32]);
@@ -500,7 +522,7 @@ __global__ void __launch_bounds__(ROW_THREADS) mx4_row_kernel(const RowParams p)
               neg = __dp4a((int)lookup((x >> 16) ^ 0x8888u), ah, neg);
             }
             // (the sum meets one scale after the other: their product alone may leave fp32's range)
-            sum[t] += (float)(pos - neg) * s_sc[t][(i - first) * NB + h] * scale_value<FMT>(h ? sb >> 8 : sb & 0xffu);
+            sum[t] += (float)(pos - neg) * s_sc[t][(i - first) * NB + h] * scale_value<FMT>(h ? cur_sb[k] >> 8 : cur_sb[k] & 0xffu);
           }
         }
       }
@@ -518,7 +540,7 @@ __global__ void __launch_bounds__(ROW_THREADS) mx4_row_kernel(const RowParams p)
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       sum[t] = 0.f;
-      for (int k = 0; k < ROW_THREADS / 32; ++k) sum[t] += s_part[k][t];
+      for (int k = 0; k < LPR / 32; ++k) sum[t] += s_part[tid / LPR * (LPR / 32) + k][t];
     }
   }
   if (row_ok && at0 == 0) {
@@ -599,9 +621,9 @@ cudaError_t tc_start(const TcParams4& p, int grid, size_t smem, cudaStream_t st)
 
 template <int FMT, int T>
 cudaError_t row_start(const RowParams& p, int b, int num_sms, cudaStream_t st) {
-  // rows enough for two CTAs of sixteen rows on every SM, or long ones would leave most of the chip idle
+  // fewer rows than that would leave SMs without a CTA of sixteen of them
   if (p.N >= num_sms * 4) return launch_kernel(mx4_row_kernel<FMT, T, 16>, dim3((unsigned)((p.N + 15) / 16), (unsigned)b), dim3(ROW_THREADS), 0, st, p);
-  return launch_kernel(mx4_row_kernel<FMT, T, ROW_THREADS>, dim3((unsigned)p.N, (unsigned)b), dim3(ROW_THREADS), 0, st, p);
+  return launch_kernel(mx4_row_kernel<FMT, T, ROW_THREADS / 2>, dim3((unsigned)((p.N + 1) / 2), (unsigned)b), dim3(ROW_THREADS), 0, st, p);
 }
 template <int FMT>
 cudaError_t row_pick(const RowParams& p, int b, int num_sms, cudaStream_t st) {

@@ -6,6 +6,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAStream.h>
+#include <c10/core/ScalarTypeToTypeMeta.h>
 #include "../../include/defl.h"
 
 namespace {
@@ -116,32 +117,57 @@ Shape shape_of(int64_t b, int64_t rows, int64_t cols, int fmt) {
 }
 int side(int64_t x) { return (int)(x > DEFL_MX4_MAX_SIDE ? DEFL_MX4_MAX_SIDE + 1 : x); }
 
+int format_of(PyObject* o) {
+  const int f = !PyUnicode_Check(o) ? -1 : PyUnicode_CompareWithASCIIString(o, "mxfp4") == 0 ? DEFL_MXFP4 : PyUnicode_CompareWithASCIIString(o, "nvfp4") == 0 ? DEFL_NVFP4 : -1;
+  TORCH_CHECK_VALUE(f >= 0, "the format is mxfp4 or nvfp4");
+  return f;
+}
+
+// A part of a buffer of bytes as a contiguous tensor.
+Tensor part(const Tensor& buffer, int64_t offset, at::IntArrayRef shape, ScalarType type) {
+  auto impl = c10::make_intrusive<at::TensorImpl>(c10::Storage(buffer.storage()), c10::DispatchKeySet(c10::DispatchKey::CUDA), c10::scalarTypeToTypeMeta(type));
+  impl->set_storage_offset(offset / (int64_t)c10::elementSize(type));
+  impl->set_sizes_contiguous(shape);
+  return Tensor(std::move(impl));
+}
+
+// The tensors of a new Mx4, in one allocation.
 struct Made {
   Tensor codes, scales, scale;
   defl_mx4 ref;
   Made(int64_t b, int64_t rows, int64_t cols, int fmt, int device) {
     const Shape s = shape_of(b, rows, cols, fmt);
-    codes = make(s.codes, at::kByte, device);
-    scales = make(s.scales, at::kByte, device);
-    if (fmt == DEFL_NVFP4) scale = make({b}, at::kFloat, device);
+    const int64_t at_scales = (b * rows * s.codes[2] + 511) / 512 * 512, at_scale = at_scales + b * s.scales[1] * s.scales[2] * 512;
+    const Tensor all = make({at_scale + 4 * b}, at::kByte, device);
+    codes = part(all, 0, s.codes, at::kByte);
+    scales = part(all, at_scales, s.scales, at::kByte);
+    if (fmt == DEFL_NVFP4) scale = part(all, at_scale, {b}, at::kFloat);
     ref = {codes.data_ptr(), scales.data_ptr(), scale.defined() ? scale.data_ptr<float>() : nullptr};
   }
-  PyObject* tuple() const {
+  // as an instance of binding.Mx4, a named tuple
+  PyObject* object(PyObject* type, PyObject* fmt, int64_t rows, int64_t cols) const {
     PyObject* s = scale.defined() ? THPVariable_Wrap(scale) : Py_NewRef(Py_None);
-    return Py_BuildValue("(NNN)", THPVariable_Wrap(codes), THPVariable_Wrap(scales), s);
+    PyObject* fields = Py_BuildValue("((NNNOLL))", THPVariable_Wrap(codes), THPVariable_Wrap(scales), s, fmt, (long long)rows, (long long)cols);
+    if (!fields) throw python_error();
+    PyObject* made = PyTuple_Type.tp_new(reinterpret_cast<PyTypeObject*>(type), fields, nullptr);
+    Py_DECREF(fields);
+    if (!made) throw python_error();
+    return made;
   }
 };
 
-// mx4_quantize(handle, device, X, format, which: 1 blocks along cols, 2 along rows, 3 both) -> (tuple or None, tuple or None), or the error code
+// mx4_quantize(handle, device, X, format, which: 1 blocks along cols, 2 along rows, 3 both, Mx4) -> an Mx4 or a pair, or the error code
 PyObject* mx4_quantize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
-  TORCH_CHECK(nargs == 5, "mx4_quantize takes 5 arguments");
+  TORCH_CHECK(nargs == 6, "mx4_quantize takes 6 arguments");
+  TORCH_CHECK(PyType_Check(a[5]) && PyType_IsSubtype(reinterpret_cast<PyTypeObject*>(a[5]), &PyTuple_Type), "the last argument is a named tuple");
   defl_ctx* c = handle(a[0]);
-  const int device = (int)PyLong_AsLong(a[1]), fmt = (int)PyLong_AsLong(a[3]), which = (int)PyLong_AsLong(a[4]);
+  const int device = (int)PyLong_AsLong(a[1]), fmt = format_of(a[3]), which = (int)PyLong_AsLong(a[4]);
   const Tensor& X = tensor(a[2], "X");
   TORCH_CHECK_VALUE(X.dim() == 3 && X.is_cuda() && X.get_device() == device && (X.scalar_type() == at::kBFloat16 || X.scalar_type() == at::kFloat),
                     "X must be a bfloat16 or float32 tensor [b, rows, cols] on cuda:", device);
-  int64_t b = X.size(0), rows = X.size(1), cols = X.size(2), sr = X.stride(1), sc = X.stride(2);
+  const int64_t b = X.size(0), m = X.size(1), n = X.size(2);
+  int64_t rows = m, cols = n, sr = X.stride(1), sc = X.stride(2);
   if (b <= 0 || rows <= 0 || cols <= 0) return PyLong_FromLong(DEFL_ERR_ARG);
   if (b > 65535 || rows > DEFL_MX4_MAX_SIDE || cols > DEFL_MX4_MAX_SIDE) return PyLong_FromLong(DEFL_ERR_RANK);
   std::optional<Made> by_rows, by_cols;
@@ -164,7 +190,12 @@ PyObject* mx4_quantize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   const int rc = defl_mx4_quantize(c, X.data_ptr(), code_of(X.scalar_type()), (int)b, (int)rows, (int)cols, sr, X.stride(0), fmt, r, t,
                                    work.defined() ? work.data_ptr() : nullptr);
   if (rc) return PyLong_FromLong(rc);
-  return Py_BuildValue("(NN)", by_rows ? by_rows->tuple() : Py_NewRef(Py_None), by_cols ? by_cols->tuple() : Py_NewRef(Py_None));
+  if (which == 3) {
+    PyObject* first = by_rows->object(a[5], a[3], m, n);
+    PyObject* second = by_cols->object(a[5], a[3], n, m);
+    return Py_BuildValue("(NN)", first, second);
+  }
+  return which & 1 ? by_rows->object(a[5], a[3], m, n) : by_cols->object(a[5], a[3], n, m);
   END_HANDLE_TH_ERRORS
 }
 
@@ -192,7 +223,7 @@ PyObject* mx4_dequantize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
   TORCH_CHECK(nargs == 9, "mx4_dequantize takes 9 arguments");
   defl_ctx* c = handle(a[0]);
-  const int device = (int)PyLong_AsLong(a[1]), fmt = (int)PyLong_AsLong(a[5]), type = (int)PyLong_AsLong(a[8]);
+  const int device = (int)PyLong_AsLong(a[1]), fmt = format_of(a[5]), type = (int)PyLong_AsLong(a[8]);
   const int64_t rows = PyLong_AsLongLong(a[6]), cols = PyLong_AsLongLong(a[7]);
   int64_t b = 0;
   if (PyErr_Occurred()) throw python_error();
@@ -210,7 +241,7 @@ PyObject* mx4_gemm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
   TORCH_CHECK(nargs == 15, "mx4_gemm takes 15 arguments");
   defl_ctx* c = handle(a[0]);
-  const int device = (int)PyLong_AsLong(a[1]), fmt = (int)PyLong_AsLong(a[8]);
+  const int device = (int)PyLong_AsLong(a[1]), fmt = format_of(a[8]);
   int type = (int)PyLong_AsLong(a[13]);
   const int64_t M = PyLong_AsLongLong(a[9]), N = PyLong_AsLongLong(a[10]), K = PyLong_AsLongLong(a[11]);
   const double alpha = PyFloat_AsDouble(a[14]);

@@ -325,9 +325,11 @@ def test_refusals_and_sizes_without_a_device():
     build.build()
     L = binding.lib()
     with pytest.raises(ValueError):
-        binding._native().mx4_quantize(0, 0, torch.zeros(1, 4, 4), 0, 1)
+        binding._native().mx4_quantize(0, 0, torch.zeros(1, 4, 4), "mxfp4", 1, binding.Mx4)
+    with pytest.raises(ValueError):
+        binding._native().mx4_quantize(0, 0, torch.zeros(1, 4, 4), "fp4", 1, binding.Mx4)
     with pytest.raises(TypeError):
-        binding._native().mx4_quantize(0, 0, None, 0, 1)
+        binding._native().mx4_quantize(0, 0, None, "nvfp4", 1, binding.Mx4)
     assert L.defl_mx4_quantize(None, None, 0, 1, 1, 1, ctypes.c_int64(1), ctypes.c_int64(1), 0, None, None, None) == -1
     assert L.defl_mx4_dequantize(None, None, 1, 1, 1, 0, None, 0) == -1
     assert L.defl_mx4_gemm(None, None, None, 1, 1, 1, 1, 0, 0, ctypes.c_float(1.0), None, ctypes.c_int64(1), ctypes.c_int64(1), 0) == -1

@@ -78,13 +78,15 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t big, float whole, flo
     const float x = __uint_as_float(big) * unit, sixth = 1.f / 6.f, t = x * sixth, a = fmaf(fmaf(-t, 6.f, x), sixth, t);
     q.byte = (uint32_t)__nv_cvt_float_to_fp8(a, __NV_SATFINITE, __NV_E4M3);
     q.s = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)q.byte, __NV_E4M3))) * whole;
-    const float r = q.s > 0.f ? __frcp_rn(q.s) : 0.f;
     if (SHORT) {
-      // r in two parts, the first of 16 bits
+      // 1 / s in two parts, the first of 16 bits, the second from its exact remainder (for that an approximate 1 / s is enough)
+      float r;
+      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(q.s));
+      if (!(q.s > 0.f)) r = 0.f;
       q.r = __uint_as_float(__float_as_uint(r) & 0xffffff00u);
-      q.lo = q.s > 0.f ? fmaf(-q.r, q.s, 1.f) * r : 0.f;
+      q.lo = fmaf(-q.r, q.s, 1.f) * r;
     } else {
-      q.r = r;
+      q.r = q.s > 0.f ? __frcp_rn(q.s) : 0.f;
     }
     if (big >= 0x7f800000u) q.byte = 0x7fu;
   }
@@ -140,12 +142,20 @@ __global__ void __launch_bounds__(Q_THREADS) mx4_quantize_kernel(const QuantPara
   if (VEC) {
     constexpr int PER = TILE * ES / 16;          // 16-byte pieces a row
     const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem);
+    constexpr int ROWS = Q_THREADS / PER;        // rows a pass of the CTA covers
+    const int r0 = tid / PER, c = (tid % PER) * (16 / ES);
+    const uint32_t dst = base + 4 * row_word<T>(r0) + (tid % PER) * 16;
+    const T* src = X + (long long)(row0 + r0) * p.ld + col0 + c;
+    if (row0 + TILE <= p.rows && col0 + TILE <= p.cols) {
 #pragma unroll
-    for (int i = 0; i < TILE * PER / Q_THREADS; ++i) {
-      const int u = tid + Q_THREADS * i, r = u / PER, c = (tid % PER) * (16 / ES);
-      int left = row0 + r < p.rows ? (p.cols - col0 - c) * ES : 0;
-      left = left < 0 ? 0 : left > 16 ? 16 : left;
-      copy16(base + 4 * row_word<T>(r) + (tid % PER) * 16, left ? X + (long long)(row0 + r) * p.ld + col0 + c : X, (uint32_t)left);
+      for (int i = 0; i < TILE / ROWS; ++i, src += (long long)ROWS * p.ld) copy16(dst + 4 * row_word<T>(ROWS * i), src, 16u);
+    } else {
+#pragma unroll
+      for (int i = 0; i < TILE / ROWS; ++i, src += (long long)ROWS * p.ld) {
+        int left = row0 + r0 + ROWS * i < p.rows ? (p.cols - col0 - c) * ES : 0;
+        left = left < 0 ? 0 : left > 16 ? 16 : left;
+        copy16(dst + 4 * row_word<T>(ROWS * i), left ? src : X, (uint32_t)left);
+      }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   } else {

@@ -15,8 +15,8 @@ namespace {
 
 constexpr int OPT_THREADS = 256;
 constexpr int CHUNK = 2048;                       // elements of one CTA's trip: 8 a thread, a block of 256 a warp
-constexpr int ADAM_CAP = 440, ADAM_CAP_SMALL = 48;   // tensors a launch: 440 x 72 bytes fill the 32,764 bytes of parameters
-constexpr int NORM_CAP = 1300, NORM_CAP_SMALL = 160;
+constexpr int ADAM_CAP = 440, ADAM_CAP_SMALL = 48, ADAM_CAP_MID = 160;   // tensors a launch: 440 x 72 bytes fill the 32,764 bytes of parameters
+constexpr int NORM_CAP = 1300, NORM_CAP_MID = 440, NORM_CAP_SMALL = 48;      // (a launch copies its parameters whole)
 constexpr int NORM_BLOCKS = 592;                  // four CTAs on each of 148 SMs
 constexpr int NORM_CHUNK = 4 * CHUNK;
 
@@ -41,6 +41,19 @@ struct AdamTable {
   AdamTensor t[CAP];
 };
 static_assert(sizeof(AdamTable<ADAM_CAP>) <= 32764, "kernel parameters");
+
+// The last tensor, from number i on, that starts at or before this chunk. (Mostly number i itself; else by halves: a walk through
+// hundreds of small tensors behind a large one took 20 us.)
+template <typename Table>
+__device__ __forceinline__ int find_tensor(const Table& tb, int i, unsigned int chunk) {
+  int hi = tb.count - 1;
+  if (i >= hi || tb.t[i + 1].first > chunk) return i;
+  for (++i; i < hi;) {
+    const int mid = (i + hi + 1) >> 1;
+    if (tb.t[mid].first <= chunk) i = mid; else hi = mid - 1;
+  }
+  return i;
+}
 
 // the mixing function of defl_fill_gaussian's generator
 __host__ __device__ __forceinline__ unsigned long long mix64(unsigned long long x) {
@@ -268,15 +281,7 @@ __global__ void __launch_bounds__(OPT_THREADS, 4) adamw_kernel(const __grid_cons
   __shared__ unsigned long long key_base;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   unsigned int chunk = blockIdx.x;
-  int i = 0;
-  {
-    int lo = 0, hi = tb.count - 1;                 // the last tensor that starts at or before this chunk
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (tb.t[mid].first <= chunk) lo = mid; else hi = mid - 1;
-    }
-    i = lo;
-  }
+  int i = find_tensor(tb, 0, chunk);
   pdl_wait();
   if (warp == 0) {
     const AdamHyper& h = tb.h;
@@ -297,7 +302,7 @@ __global__ void __launch_bounds__(OPT_THREADS, 4) adamw_kernel(const __grid_cons
   const Scalars s = sc;
   if (s.c == 0.f) return;                          // gradients that were not finite: the step is left out
   for (; chunk < tb.chunks; chunk += gridDim.x) {
-    while (i + 1 < tb.count && tb.t[i + 1].first <= chunk) ++i;
+    i = find_tensor(tb, i, chunk);
     const AdamTensor& t = tb.t[i];
     const long long base = (long long)(chunk - t.first) * CHUNK + warp * 256, left = t.n - base;      // this warp's block
     if (left <= 0) continue;
@@ -355,12 +360,7 @@ __global__ void __launch_bounds__(OPT_THREADS) grad_norm_kernel(const __grid_con
   double acc = 0.0;
   int i = 0;
   for (unsigned int chunk = blockIdx.x; chunk < tb.chunks; chunk += gridDim.x) {
-    int lo = i, hi = tb.count - 1;                 // the last tensor that starts at or before this chunk
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (tb.t[mid].first <= chunk) lo = mid; else hi = mid - 1;
-    }
-    i = lo;
+    i = find_tensor(tb, i, chunk);
     const NormTensor& t = tb.t[i];
     const long long base = (long long)(chunk - t.first) * NORM_CHUNK + threadIdx.x * 8;
     const long long left = t.n - base;
@@ -519,8 +519,10 @@ int defl_adamw_step(defl_ctx* c, const defl_adamw_tensor* t, int count, const de
         tb.chunks += (unsigned int)((x.n + CHUNK - 1) / CHUNK);
       }
       if (tb.count == 0) break;
-      const cudaError_t e = tb.count <= ADAM_CAP_SMALL ? adamw_type<ADAM_CAP_SMALL>(tb, cls, o->stochastic != 0, c->num_sms, c->stream)
-                                                       : adamw_type<ADAM_CAP>(tb, cls, o->stochastic != 0, c->num_sms, c->stream);
+      const bool sr = o->stochastic != 0;
+      const cudaError_t e = tb.count <= ADAM_CAP_SMALL ? adamw_type<ADAM_CAP_SMALL>(tb, cls, sr, c->num_sms, c->stream)
+                            : tb.count <= ADAM_CAP_MID ? adamw_type<ADAM_CAP_MID>(tb, cls, sr, c->num_sms, c->stream)
+                                                       : adamw_type<ADAM_CAP>(tb, cls, sr, c->num_sms, c->stream);
       ++c->launches;
       if (ctx_fail(c, e, "adamw")) return DEFL_ERR_CUDA;
     }
@@ -561,7 +563,8 @@ int defl_grad_norm(defl_ctx* c, const defl_norm_tensor* t, int count, float max_
     const int grid = tb.chunks < (unsigned int)NORM_BLOCKS ? (int)tb.chunks : NORM_BLOCKS;
     tb.partial = partial + slots;
     slots += grid;
-    const cudaError_t e = tb.count <= NORM_CAP_SMALL ? norm_launch<NORM_CAP_SMALL>(tb, grid, c->stream) : norm_launch<NORM_CAP>(tb, grid, c->stream);
+    const cudaError_t e = tb.count <= NORM_CAP_SMALL ? norm_launch<NORM_CAP_SMALL>(tb, grid, c->stream)
+                          : tb.count <= NORM_CAP_MID ? norm_launch<NORM_CAP_MID>(tb, grid, c->stream) : norm_launch<NORM_CAP>(tb, grid, c->stream);
     ++c->launches;
     if (ctx_fail(c, e, "grad norm")) return DEFL_ERR_CUDA;
   }

@@ -46,7 +46,7 @@ struct TcParams4 {
   int tiles_m, tiles_n;
   int total_tiles;
   int kblocks, ksteps_last;                        // stages a tile, and products of 64 values in the last of them
-  int stages, sets, overlap, stg_bufs;
+  int stages, sets, overlap;
   uint32_t a_bytes, b_bytes, stage_bytes;
   uint32_t idesc;
   int out_f32, store_tma;
@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
     const uint32_t full0 = PAIR ? map_to_cta(smem_u32(&full_bar[0]), 0) : smem_u32(&full_bar[0]);
     const uint32_t sf_col = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + SF_COL;
     constexpr uint32_t SLOT = (1u + NSB) * ATOMS * 512u;
-    const uint32_t ring = smem_base + (uint32_t)p.stages * p.stage_bytes + (uint32_t)(TC_EPI_WARPS * p.stg_bufs) * STG_BYTES;
+    const uint32_t ring = smem_base + (uint32_t)p.stages * p.stage_bytes + (uint32_t)TC_EPI_WARPS * STG_BYTES;
     uint32_t slot = 0, phase = 0, set = 0, stage = 0, old = 0, old_phase = 0;
     int step = 0;
     bool live = true;
@@ -308,10 +308,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
   } else {
     // ------------------------------------------------------------------ read-out: 32 rows and every other chunk of columns a warp
     const int q = warp & 3, wsel = (warp - 2) >> 2;
-    const uint32_t stg0 = smem_base + (uint32_t)p.stages * p.stage_bytes + (uint32_t)((warp - 2) * p.stg_bufs) * STG_BYTES;
+    const uint32_t stg = smem_base + (uint32_t)p.stages * p.stage_bytes + (uint32_t)(warp - 2) * STG_BYTES;
+    const uint32_t empty_sig = PAIR ? map_to_cta(smem_u32(&acc_empty_bar[0]), 0) : smem_u32(&acc_empty_bar[0]);
     const uint32_t ovl_sig = PAIR ? map_to_cta(smem_u32(&ovl_bar), 0) : smem_u32(&ovl_bar);
     const int cw = p.out_f32 ? 32 : 64;            // columns of 128 bytes
-    int buf = 0;
     pdl_wait();
     for (int tile = tile0, it = 0; tile < p.total_tiles; tile += tile_step, ++it) {
       const Tile4 t = tile_of<PAIR>(p, tile);
@@ -323,27 +323,36 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (acc ? acc1 : 0u);
       const int row0 = t.tm * TILE_M + (int)rank * 128 + q * 32, n0 = t.tn * p.BN;
       const int chunks = (t.n_eff + cw - 1) / cw, ovl_chunks = (p.overlap + cw - 1) / cw, full = p.BN / cw;
-      bool told = !p.overlap;
-      // the overlapping columns come first: the last ones of the first accumulator, the first ones of the second
-      for (int i = wsel; i < full; i += 2) {
-        if (!told && i >= ovl_chunks) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) { if (PAIR) mbar_arrive_cluster(ovl_sig); else mbar_arrive(ovl_sig); }
-          told = true;
+      // What has left tensor memory is given back at once, before it is packed and stored: the overlapping columns, which come first (the
+      // last ones of the first accumulator, the first ones of the second), then the rest.
+      auto tell = [&](bool both, bool accumulator) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (both) { if (PAIR) mbar_arrive_cluster(ovl_sig); else mbar_arrive(ovl_sig); }
+          if (accumulator) { if (PAIR) mbar_arrive_cluster(empty_sig + 8u * acc); else mbar_arrive(empty_sig + 8u * acc); }
         }
+        __syncwarp();
+      };
+      bool told = !p.overlap;
+      if (wsel >= full || (!told && wsel >= ovl_chunks)) { tell(!told, wsel >= full); told = true; }
+      for (int i = wsel; i < full; i += 2) {
         const int c = (p.overlap && acc == 0) ? full - 1 - i : i;
-        if (c >= chunks || row0 >= p.M) continue;
+        const bool active = c < chunks && row0 < p.M;
         const int col0 = c * cw;
         uint32_t r[64];
-        tmem_ld32(taddr + col0, r);
-        if (!p.out_f32) tmem_ld32(taddr + col0 + 32, r + 32);
-        const uint32_t stg = stg0 + (uint32_t)buf * STG_BYTES;
-        // the buffer's last store has read it
-        if (p.stg_bufs == 2) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-        else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        if (active) {
+          tmem_ld32(taddr + col0, r);
+          if (!p.out_f32) tmem_ld32(taddr + col0 + 32, r + 32);
+          tmem_ld_wait();
+        }
+        const bool ovl_now = !told && i + 2 >= ovl_chunks, last = i + 2 >= full;
+        if (ovl_now || last) tell(ovl_now, last);
+        told = told || ovl_now;
+        if (!active) continue;
+        // the last store has read the buffer
+        asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
         __syncwarp();
-        tmem_ld_wait();
 #pragma unroll
         for (int pc = 0; pc < 8; ++pc) {
           uint32_t w[4];
@@ -380,15 +389,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
           }
           __syncwarp();
         }
-        if (p.stg_bufs == 2) buf ^= 1;
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        if (!told) { if (PAIR) mbar_arrive_cluster(ovl_sig); else mbar_arrive(ovl_sig); }
-        if (PAIR) mbar_arrive_cluster(map_to_cta(smem_u32(&acc_empty_bar[acc]), 0)); else mbar_arrive(smem_u32(&acc_empty_bar[acc]));
-      }
-      __syncwarp();
     }
     asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");       // what is on its way to memory gets there before the CTA ends
   }
@@ -680,8 +681,7 @@ cudaError_t mx4_gemm_launch(const Mx4Gemm& g, cudaStream_t st, int* status, int 
   const uint32_t b_rows = (uint32_t)(pair ? p.BN / 2 : p.BN);
   p.a_bytes = 128 * KB_BYTES; p.b_bytes = b_rows * KB_BYTES;
   p.stage_bytes = p.a_bytes + p.b_bytes;
-  p.stg_bufs = 1;
-  const uint32_t ring = (uint32_t)(scale_ring(g.fmt) * (1 + nsb) * atoms) * 512u, stg = (uint32_t)(TC_EPI_WARPS * p.stg_bufs) * STG_BYTES, room = SMEM_MOST - 1024 - 1024 - stg - ring;
+  const uint32_t ring = (uint32_t)(scale_ring(g.fmt) * (1 + nsb) * atoms) * 512u, stg = (uint32_t)TC_EPI_WARPS * STG_BYTES, room = SMEM_MOST - 1024 - 1024 - stg - ring;
   p.stages = (int)(room / p.stage_bytes);
   if (p.stages > MAX_ST) p.stages = MAX_ST;
   p.sets = p.stages < SF_SETS ? p.stages : SF_SETS;

@@ -63,3 +63,18 @@ def muon_step_groups(ctx, weights, momenta, grads, lr, mu, window, oversample, p
         k = int(math.ceil(window * ms)) if 0 < window < 1 else int(window)
         p = int(math.ceil(oversample * ms)) if 0 < oversample < 1 else int(oversample)
         ctx.defl_muon_step_batched(W, momenta[shape], grads.get(shape), lr, mu, k, p, power_iters, coeff_schedule, **kw)
+
+
+def optimizer_step_groups(ctx, weights, momenta, grads, lr, mu, window, oversample, power_iters, coeff_schedule, rest, rest_grads, rest_lr,
+                          rest_step, max_norm=0.0, adamw=None, **kw):
+    """One optimizer step over a whole model: Muon on the stacked matrix groups (as muon_step_groups; kw goes there) and AdamW
+    on the rest, a binding.AdamWGroup with one gradient per tensor (None: left alone). The global norm is taken over all
+    gradients together; with max_norm > 0 its factor scales both kinds. rest_step is an int64 CUDA tensor [1], the number of
+    AdamW steps taken so far: it is advanced on the device. A norm that is not finite leaves the rest and the counter as they are,
+    and the matrices take a step along their momentum without the gradient. `adamw`: further arguments of defl_adamw_step.
+    Nothing waits; returns the tensor (norm, factor)."""
+    every = [g for g in grads.values() if g is not None] + [g for g in rest_grads if g is not None]
+    clip = ctx.defl_grad_norm(every, max_norm, step=rest_step)
+    muon_step_groups(ctx, weights, momenta, grads, lr, mu, window, oversample, power_iters, coeff_schedule, grad_scale=clip, **kw)
+    ctx.defl_adamw_step(rest, rest_grads, rest_lr, rest_step, grad_scale=clip, **(adamw or {}))
+    return clip

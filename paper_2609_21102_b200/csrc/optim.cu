@@ -15,7 +15,7 @@ namespace {
 
 constexpr int OPT_THREADS = 256;
 constexpr int CHUNK = 2048;                       // elements of one CTA's trip: 8 a thread, a block of 256 a warp
-constexpr int ADAM_CAP = 440, ADAM_CAP_SMALL = 48, ADAM_CAP_MID = 160;   // tensors a launch: 440 x 72 bytes fill the 32,764 bytes of parameters
+constexpr int ADAM_CAP = 438, ADAM_CAP_SMALL = 48, ADAM_CAP_MID = 160;   // tensors a launch: 438 x 72 bytes fill the 32,764 bytes of parameters
 constexpr int NORM_CAP = 1300, NORM_CAP_MID = 440, NORM_CAP_SMALL = 48;      // (a launch copies its parameters whole)
 constexpr int NORM_BLOCKS = 592;                  // four CTAs on each of 148 SMs
 constexpr int NORM_CHUNK = 4 * CHUNK;
@@ -32,6 +32,9 @@ struct AdamHyper {
   const long long* step_dev; const float* lr_dev; const float* grad_scale;
   unsigned long long seed;     // the generator's h(seed)
   float b1, ob1, b2, ob2, eps;
+  int known;                   // step and learning rate came from the host: what follows from them is here already
+  float size, rc2, keep;
+  unsigned long long key_base;
 };
 template <int CAP>
 struct AdamTable {
@@ -278,28 +281,32 @@ __device__ __forceinline__ void adam_block(const AdamTensor& t, const AdamHyper&
 template <typename P, typename G, bool EIGHT, bool SR, int CAP>
 __global__ void __launch_bounds__(OPT_THREADS, 4) adamw_kernel(const __grid_constant__ AdamTable<CAP> tb) {
   __shared__ Scalars sc;
-  __shared__ unsigned long long key_base;
+  __shared__ unsigned long long shared_key;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const AdamHyper& h = tb.h;
   unsigned int chunk = blockIdx.x;
   int i = find_tensor(tb, 0, chunk);
   pdl_wait();
-  if (warp == 0) {
-    const AdamHyper& h = tb.h;
-    const long long t0 = h.step_dev ? *h.step_dev : h.step, t = t0 > 0 ? t0 : 1;
-    // two lanes, one correction each
-    const double corr = 1.0 - power_of(lane == 0 ? h.beta1 : h.beta2, t);
-    const double lr = h.lr_dev ? (double)*h.lr_dev : h.lr;
-    if (lane == 0) {
-      sc.size = (float)(lr / corr);
-      sc.keep = (float)(1.0 - lr * h.decay);
-      sc.c = h.grad_scale ? *h.grad_scale : 1.f;
-      key_base = mix64(h.seed ^ (unsigned long long)t);
-    } else if (lane == 1) {
-      sc.rc2 = (float)(1.0 / sqrt(corr));
+  Scalars s = {h.size, h.rc2, h.keep, h.grad_scale ? *h.grad_scale : 1.f};
+  unsigned long long key_base = h.key_base;
+  if (!h.known) {
+    if (warp == 0) {
+      const long long t0 = h.step_dev ? *h.step_dev : h.step, t = t0 > 0 ? t0 : 1;
+      // two lanes, one correction each
+      const double corr = 1.0 - power_of(lane == 0 ? h.beta1 : h.beta2, t);
+      const double lr = h.lr_dev ? (double)*h.lr_dev : h.lr;
+      if (lane == 0) {
+        sc.size = (float)(lr / corr);
+        sc.keep = (float)(1.0 - lr * h.decay);
+        shared_key = mix64(h.seed ^ (unsigned long long)t);
+      } else if (lane == 1) {
+        sc.rc2 = (float)(1.0 / sqrt(corr));
+      }
     }
+    __syncthreads();
+    s.size = sc.size; s.rc2 = sc.rc2; s.keep = sc.keep;
+    key_base = shared_key;
   }
-  __syncthreads();
-  const Scalars s = sc;
   if (s.c == 0.f) return;                          // gradients that were not finite: the step is left out
   for (; chunk < tb.chunks; chunk += gridDim.x) {
     i = find_tensor(tb, i, chunk);
@@ -502,6 +509,15 @@ int defl_adamw_step(defl_ctx* c, const defl_adamw_tensor* t, int count, const de
   h.beta1 = o->beta1; h.beta2 = o->beta2; h.lr = o->lr; h.decay = o->weight_decay;
   h.step = o->step; h.step_dev = reinterpret_cast<const long long*>(o->step_dev); h.lr_dev = o->lr_dev; h.grad_scale = o->grad_scale;
   h.seed = mix64(o->seed);
+  h.known = !o->step_dev && !o->lr_dev;
+  h.size = h.rc2 = h.keep = 0.f;
+  h.key_base = 0;
+  if (h.known) {
+    h.size = (float)(o->lr / (1.0 - power_of(o->beta1, o->step)));
+    h.rc2 = (float)(1.0 / sqrt(1.0 - power_of(o->beta2, o->step)));
+    h.keep = (float)(1.0 - o->lr * o->weight_decay);
+    h.key_base = mix64(h.seed ^ (unsigned long long)o->step);
+  }
   h.b1 = (float)o->beta1; h.ob1 = (float)(1.0 - o->beta1); h.b2 = (float)o->beta2; h.ob2 = (float)(1.0 - o->beta2); h.eps = (float)o->eps;
   for (int cls = 0; cls < 8; ++cls) {
     if (!(present >> cls & 1u)) continue;

@@ -96,6 +96,18 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* tm, uint32_t src
                ::"l"(tm), "r"(src), "r"(c0), "r"(c1), "r"(c2) : "memory");
 }
 
+__device__ __forceinline__ uint32_t ld_word(uint32_t saddr) {
+  uint32_t w;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(saddr));
+  return w;
+}
+// element e of a staged row (its 16-byte pieces exchanged by `key`) to the row's place in memory
+__device__ __forceinline__ void copy_element(uint8_t* d, uint32_t src, uint32_t key, int e, int es) {
+  const uint32_t at = (uint32_t)(e * es), w = ld_word(src + ((at >> 4 ^ key) << 4) + (at & 12u));
+  if (es == 4) *reinterpret_cast<uint32_t*>(d + at) = w;
+  else *reinterpret_cast<uint16_t*>(d + at) = (uint16_t)(at & 2u ? w >> 16 : w);
+}
+
 struct Tile4 { int bz, tm, tn, n_eff; };
 template <int PAIR>
 __device__ __forceinline__ Tile4 tile_of(const TcParams4& p, int tile) {
@@ -374,17 +386,29 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
           }
         } else {
-          // rows that the copy engine cannot address: 4 bytes of a row a lane, single elements
+          // Rows that the copy engine cannot address: eight lanes a row, four rows at a time; the whole 16-byte pieces that the row has in
+          // memory, put together from the staged row, then the elements before and after them, one a lane. (A store takes some ten
+          // cycles of the SM whatever it writes: with 4 bytes a lane 4096 x 4097 took 32 us.)
           __syncwarp();
-          for (int rr = 0; rr < 32 && row0 + rr < p.M; ++rr) {
-            uint32_t w;
-            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(stg + (uint32_t)rr * 128u + ((uint32_t)((lane >> 2) ^ (rr & 7)) << 4) + 4u * (lane & 3)));
-            const long long at = (long long)t.bz * p.batch_d + (long long)(row0 + rr) * p.ldd + n0 + col0;
-            if (p.out_f32) {
-              if (n0 + col0 + lane < p.N) reinterpret_cast<uint32_t*>(p.D)[at + lane] = w;
+          const int rows = min(32, p.M - row0), have = min(cw, p.N - n0 - col0), es = p.out_f32 ? 4 : 2, sub = lane & 7;
+          const long long step = 4 * p.ldd * es;
+          uint8_t* d = reinterpret_cast<uint8_t*>(p.D) + ((long long)t.bz * p.batch_d + (long long)(row0 + (lane >> 3)) * p.ldd + n0 + col0) * es;
+          for (int r = lane >> 3; r < rows; r += 4, d += step) {
+            const uint32_t src = stg + (uint32_t)r * 128u, key = (uint32_t)(r & 7);
+            const uint32_t before = (16u - (uint32_t)(reinterpret_cast<uintptr_t>(d) & 15u)) & 15u;      // bytes in front of the first whole piece
+            if (have == cw) {
+              if (sub < (before ? 7 : 8)) {
+                const uint32_t first = (before >> 2) + 4u * sub, odd = (before & 2u) * 8u;
+                uint32_t a[5];
+#pragma unroll
+                for (uint32_t k = 0; k < 5; ++k) a[k] = k < 4 || odd ? ld_word(src + (((first + k) >> 2 ^ key) << 4) + ((first + k) & 3u) * 4u) : 0u;
+                *reinterpret_cast<uint4*>(d + before + 16 * sub) = make_uint4(__funnelshift_r(a[0], a[1], odd), __funnelshift_r(a[1], a[2], odd),
+                                                                              __funnelshift_r(a[2], a[3], odd), __funnelshift_r(a[3], a[4], odd));
+              }
+              const int ends = before ? 16 / es : 0, heads = (int)before / es;
+              if (sub < ends) copy_element(d, src, key, sub < heads ? sub : cw - ends + sub, es);
             } else {
-              if (n0 + col0 + 2 * lane < p.N) reinterpret_cast<uint16_t*>(p.D)[at + 2 * lane] = (uint16_t)w;
-              if (n0 + col0 + 2 * lane + 1 < p.N) reinterpret_cast<uint16_t*>(p.D)[at + 2 * lane + 1] = (uint16_t)(w >> 16);
+              for (int e = sub; e < have; e += 8) copy_element(d, src, key, e, es);
             }
           }
           __syncwarp();

@@ -419,12 +419,15 @@ int defl_mx4_quantize(defl_ctx* ctx, const void* X, int dtype, int b, int rows, 
 int defl_mx4_dequantize(defl_ctx* ctx, const defl_mx4* a, int b, int rows, int cols, int fmt, void* out, int dtype);
 
 /* D [b, M, N] = alpha A B^T with A [b, M, K] and B [b, N, K], or one B for all (b_shared != 0), of the same format; D row-major with row
- * stride ldd >= N and a batch stride of its own, DEFL_BF16 or DEFL_F32. Products are exact, sums are fp32, one rounding to bf16.
+ * stride ldd >= N and a batch stride of its own, DEFL_BF16 or DEFL_F32, apart from A and B. Products are exact, sums are fp32, one rounding to bf16.
  * Up to eight rows of A (single tokens) the weights stream through integer products, else the tensor cores take the
  * scales with the codes (tcgen05 block-scaled products). A device-side wait that runs out is reported by
  * defl_device_wait_status. Errors as defl_mx4_quantize. */
 int defl_mx4_gemm(defl_ctx* ctx, const defl_mx4* A, const defl_mx4* B, int b, int M, int N, int K, int b_shared, int fmt, float alpha, void* D,
-                  int64_t ldd, int64_t batch_stride, int out_dtype);
+                  int64_t ldd, int64_t batch_stride, int out_dtype, void* work);
+/* Bytes of `work` with which a product of few tiles and a long K is computed in parts (0: it would not be). work, device, 16-byte
+ * aligned, is of this call alone until it is through; NULL: not in parts. */
+size_t defl_mx4_gemm_work_bytes(defl_ctx* ctx, int b, int M, int N, int K, int out_dtype);
 
 /* Diagnostics: one batched product C[b,M,N] = alpha * opA(A) opB(B) through a chosen engine, used by the
  * tests to check the tensor-core tile engine against the fp32 engine (no counterpart in the paper).

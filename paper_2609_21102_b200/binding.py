@@ -32,7 +32,7 @@ EXPORTS = [
     "defl_polar_window", "defl_psd_window", "defl_polar_batched", "defl_polar_batched_host", "defl_muon_step_batched", "defl_brsvd_batched", "defl_psd_project", "defl_inv_root", "defl_admm_diag_sdp", "defl_fill_gaussian", "defl_debug_gemm",
     "defl_frobenius_norms_noalloc", "defl_set_profiling", "defl_get_stage_ms", "defl_get_stage_ms_sum", "defl_launch_count", "defl_device_wait_status",
     "defl_status_string", "defl_last_error", "defl_adamw_step", "defl_grad_norm", "defl_grad_norm_work_bytes",
-    "defl_mx4_codes_bytes", "defl_mx4_scales_bytes", "defl_mx4_work_bytes", "defl_mx4_quantize", "defl_mx4_dequantize", "defl_mx4_gemm",
+    "defl_mx4_codes_bytes", "defl_mx4_scales_bytes", "defl_mx4_work_bytes", "defl_mx4_quantize", "defl_mx4_dequantize", "defl_mx4_gemm", "defl_mx4_gemm_work_bytes",
 ]
 
 
@@ -99,6 +99,8 @@ def lib():
                                       ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_float, ctypes.c_int]
         L.defl_grad_norm_work_bytes.restype = ctypes.c_size_t
         L.defl_mx4_codes_bytes.restype = L.defl_mx4_scales_bytes.restype = L.defl_mx4_work_bytes.restype = ctypes.c_size_t
+        L.defl_mx4_gemm_work_bytes.restype = ctypes.c_size_t
+        L.defl_mx4_gemm_work_bytes.argtypes = [ctypes.c_void_p] + [ctypes.c_int] * 5
         L.defl_set_profiling.argtypes = [ctypes.c_void_p, ctypes.c_int]
         L.defl_get_stage_ms.argtypes = [ctypes.c_void_p, ctypes.POINTER(ctypes.c_float), ctypes.c_int]
         L.defl_get_stage_ms_sum.argtypes = [ctypes.c_void_p, ctypes.POINTER(ctypes.c_float), ctypes.c_int, ctypes.c_int]

@@ -597,12 +597,18 @@ int defl_mx4_dequantize(defl_ctx* c, const defl_mx4* a, int b, int rows, int col
   return DEFL_OK;
 }
 
+size_t defl_mx4_gemm_work_bytes(defl_ctx* c, int b, int M, int N, int K, int out_dtype) {
+  if (!c || b <= 0 || M <= 0 || N <= 0 || K <= 0 || b > 65535 || M > DEFL_MX4_MAX_SIDE || N > DEFL_MX4_MAX_SIDE || K > DEFL_MX4_MAX_SIDE) return 0;
+  return mx4_gemm_split(b, M, N, K, out_dtype, c->num_sms).work_bytes;
+}
+
 int defl_mx4_gemm(defl_ctx* c, const defl_mx4* A, const defl_mx4* B, int b, int M, int N, int K, int b_shared, int fmt, float alpha, void* D, int64_t ldd,
-                  int64_t batch_stride, int out_dtype) {
+                  int64_t batch_stride, int out_dtype, void* work) {
   if (!c || !A || !B || !D || b <= 0 || M <= 0 || N <= 0 || K <= 0 || ldd < N) return DEFL_ERR_ARG;
   if (b > 1 && batch_stride < (int64_t)(M - 1) * ldd + N) return DEFL_ERR_ARG;
   if ((fmt != DEFL_MXFP4 && fmt != DEFL_NVFP4) || (out_dtype != DEFL_BF16 && out_dtype != DEFL_F32)) return DEFL_ERR_ARG;
   if (!matrix_ok(A, fmt) || !matrix_ok(B, fmt) || !on(D, (unsigned)dtype_size(out_dtype))) return DEFL_ERR_ARG;
+  if (work && !on(work, 16)) return DEFL_ERR_ARG;
   if (M > DEFL_MX4_MAX_SIDE || N > DEFL_MX4_MAX_SIDE || K > DEFL_MX4_MAX_SIDE || b > 65535) return DEFL_ERR_RANK;
   DeviceScope scope(c->device);
   c->err[0] = 0;
@@ -610,7 +616,7 @@ int defl_mx4_gemm(defl_ctx* c, const defl_mx4* A, const defl_mx4* B, int b, int 
   g.A = {(const uint8_t*)A->codes, (const uint8_t*)A->scales, A->scale};
   g.B = {(const uint8_t*)B->codes, (const uint8_t*)B->scales, B->scale};
   g.b = b; g.M = M; g.N = N; g.K = K; g.fmt = fmt; g.b_shared = b_shared != 0;
-  g.D = D; g.ldd = ldd; g.batch_d = batch_stride; g.out_dtype = out_dtype; g.alpha = alpha;
+  g.D = D; g.ldd = ldd; g.batch_d = batch_stride; g.out_dtype = out_dtype; g.alpha = alpha; g.work = work;
   const unsigned long long wait_ns = (unsigned long long)(c->tc_knobs.wait_ms > 0 ? c->tc_knobs.wait_ms : 2000) * 1000000ull;
   if (ctx_fail(c, mx4_gemm_launch(g, c->stream, c->wait_status, c->num_sms, wait_ns, &c->launches), "mx4 gemm")) return DEFL_ERR_CUDA;
   return DEFL_OK;

@@ -20,7 +20,11 @@ struct Mx4Gemm {
   int b, M, N, K, fmt, b_shared;
   void* D; long long ldd, batch_d; int out_dtype;
   float alpha;
+  void* work;                  // room for the parts of a product that is split along K, or null: not split
 };
+// How many parts of K a product of these sizes is best computed in, and the room that takes.
+struct Mx4Split { int splits; size_t work_bytes; };
+Mx4Split mx4_gemm_split(int b, int M, int N, int K, int out_dtype, int num_sms);
 cudaError_t mx4_gemm_prepare();
 cudaError_t mx4_quantize_prepare();
 cudaError_t mx4_gemm_launch(const Mx4Gemm& g, cudaStream_t st, int* status, int num_sms, unsigned long long wait_ns, long long* launches);

@@ -45,7 +45,8 @@ struct TcParams4 {
   int M, N, batch, BN, b_shared;
   int tiles_m, tiles_n;
   int total_tiles;
-  int kblocks, ksteps_last;                        // stages a tile, and products of 64 values in the last of them
+  int kblocks, ksteps_last;                        // stages of K, and products of 64 values in the last of them
+  int splits, kper;                                // parts of K that are tiles of their own, stages each; D is then [splits, batch, M, N]
   int stages, sets, overlap;
   uint32_t a_bytes, b_bytes, stage_bytes;
   uint32_t idesc;
@@ -108,13 +109,16 @@ __device__ __forceinline__ void copy_element(uint8_t* d, uint32_t src, uint32_t 
   else *reinterpret_cast<uint16_t*>(d + at) = (uint16_t)(at & 2u ? w >> 16 : w);
 }
 
-struct Tile4 { int bz, tm, tn, n_eff; };
+struct Tile4 { int bz, tm, tn, n_eff, ks, k0, k1; };      // k0 .. k1: the stages of this part of K
 template <int PAIR>
 __device__ __forceinline__ Tile4 tile_of(const TcParams4& p, int tile) {
   Tile4 t;
   const int per = p.tiles_m * p.tiles_n;
-  t.bz = tile / per;
-  const int i = tile - t.bz * per;
+  const int z = tile / per, i = tile - z * per;
+  t.ks = p.splits > 1 ? z / p.batch : 0;
+  t.bz = z - t.ks * p.batch;
+  t.k0 = t.ks * p.kper;
+  t.k1 = min(t.k0 + p.kper, p.kblocks);
   t.tn = i / p.tiles_m;                            // tiles of one column of tiles follow one another: they share B
   t.tm = i - t.tn * p.tiles_m;
   const int left = p.N - t.tn * p.BN, q = PAIR ? 31 : 15;
@@ -185,7 +189,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
       const int n0 = t.tn * p.BN, m0 = t.tm * TILE_M + (int)rank * 128;
       const int bz_b = p.b_shared ? 0 : t.bz;
       const int c1 = lane == 0 ? m0 : n0 + (PAIR ? (int)rank * (t.n_eff >> 1) : 0), c2 = lane == 0 ? t.bz : bz_b;
-      for (int kb = 0; kb < p.kblocks; ++kb) {
+      for (int kb = t.k0; kb < t.k1; ++kb) {
         int ok = 1;
         if (lane == 0) ok = mbar_wait(empty0 + 8u * stage, phase ^ 1u, &abort_flag, p.status, p.wait_ns) ? 1 : 0;
         ok = __shfl_sync(0xffffffffu, ok, 0);
@@ -216,8 +220,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
         const uint32_t d = tmem_base + (acc ? acc1 : 0u);
         const uint32_t idesc = p.idesc | ((uint32_t)(t.n_eff >> 3) << 17);
         const uint32_t shift = (uint32_t)((t.tn * p.BN) & 127) >> 5;      // B's first row within its tile of scales, in columns
-        int kb = 0;
-        for (; kb < p.kblocks; ++kb) {
+        int kb = t.k0;
+        for (; kb < t.k1; ++kb) {
           if (!ready && !mbar_wait(full0 + 8u * stage, phase, &abort_flag, p.status, p.wait_ns)) break;
           tc_fence_after();
           // a look at the next stage's barrier now: a wait takes 170 cycles also where there is nothing to wait for, and this thread's
@@ -230,7 +234,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
             if (kk < ksteps) {
               const int a = FMT == MXFP4 ? kk >> 1 : kk;
               const uint32_t id = FMT == MXFP4 ? (uint32_t)(kk & 1) * 2u : 0u;
-              umma4<FMT, PAIR>(d, lo + 2u * kk, lo + b_off + 2u * kk, idesc | id << 4 | id << 29, sa + 4u * a, sb + 4u * (a * NSB), (kb | kk) ? 1u : 0u);
+              umma4<FMT, PAIR>(d, lo + 2u * kk, lo + b_off + 2u * kk, idesc | id << 4 | id << 29, sa + 4u * a, sb + 4u * (a * NSB), kb > t.k0 || kk > 0 ? 1u : 0u);
             }
           }
           // (one commit a stage, for its codes and its scales: a second one to both CTAs took 250 cycles)
@@ -238,7 +242,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
           if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
           if (++set == (uint32_t)p.sets) set = 0;
         }
-        if (kb < p.kblocks) break;
+        if (kb < t.k1) break;
         if (PAIR) umma_commit_pair(smem_u32(&acc_full_bar[acc])); else umma_commit(smem_u32(&acc_full_bar[acc]));
       }
     }
@@ -264,8 +268,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
         const int rt = lane == 0 ? (t.tm * TILE_M >> 7) + (int)rank : (t.tn * p.BN >> 7) + lane - 1, rts = lane == 0 ? p.rt_a : p.rt_b;
         const bool exists = lane < 1 + NSB && rt < rts;
         const uint32_t count = (uint32_t)__popc(__ballot_sync(0xffffffffu, exists));
-        const uint8_t* src = (lane == 0 ? p.sa : p.sb) + ((long long)(lane > 0 && p.b_shared ? 0 : t.bz) * rts + rt) * p.kt * 512;
-        for (int kb = 0; kb < p.kblocks; ++kb, src += ATOMS * 512) {
+        const uint8_t* src = (lane == 0 ? p.sa : p.sb) + ((long long)(lane > 0 && p.b_shared ? 0 : t.bz) * rts + rt) * p.kt * 512 + (long long)t.k0 * (ATOMS * 512);
+        for (int kb = t.k0; kb < t.k1; ++kb, src += ATOMS * 512) {
           const uint32_t bytes = (uint32_t)min(ATOMS, p.kt - kb * ATOMS) * 512u;
           int ok = 1;
           if (lane == 0) {
@@ -283,7 +287,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
       live = false;
     }
     for (int tile = tile0; tile < p.total_tiles && live; tile += tile_step) {
-      for (int kb = 0; kb < p.kblocks; ++kb) {
+      const Tile4 t = tile_of<PAIR>(p, tile);
+      for (int kb = t.k0; kb < t.k1; ++kb) {
         // The set is free once the products of the stage that had it before are through: no more sets than stages, so that stage's
         // barrier cannot have gone round again, and this stage's barrier counts the scales of no earlier round.
         uint32_t landed = mbar_test(land0 + 8u * slot, phase), free_set = step < p.sets || mbar_test(empty0 + 8u * old, old_phase);
@@ -329,7 +334,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
       const Tile4 t = tile_of<PAIR>(p, tile);
       const uint32_t acc = (uint32_t)it & 1u, use = ((uint32_t)it >> 1) & 1u;
       float alpha = p.alpha;
-      if (FMT == NVFP4) alpha *= p.scale_a[t.bz] * p.scale_b[p.b_shared ? 0 : t.bz];
+      if (FMT == NVFP4 && p.splits == 1) alpha *= p.scale_a[t.bz] * p.scale_b[p.b_shared ? 0 : t.bz];
+      const int out_z = t.ks * p.batch + t.bz;
       if (!mbar_wait(smem_u32(&acc_full_bar[acc]), use, &abort_flag, p.status, p.wait_ns)) break;
       tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (acc ? acc1 : 0u);
@@ -382,7 +388,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (lane == 0) {
-            if (n0 + col0 < p.N) tma_store_3d(&p.tmD, stg, n0 + col0, row0, t.bz);
+            if (n0 + col0 < p.N) tma_store_3d(&p.tmD, stg, n0 + col0, row0, out_z);
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
           }
         } else {
@@ -392,7 +398,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
           __syncwarp();
           const int rows = min(32, p.M - row0), have = min(cw, p.N - n0 - col0), es = p.out_f32 ? 4 : 2, sub = lane & 7;
           const long long step = 4 * p.ldd * es;
-          uint8_t* d = reinterpret_cast<uint8_t*>(p.D) + ((long long)t.bz * p.batch_d + (long long)(row0 + (lane >> 3)) * p.ldd + n0 + col0) * es;
+          uint8_t* d = reinterpret_cast<uint8_t*>(p.D) + ((long long)out_z * p.batch_d + (long long)(row0 + (lane >> 3)) * p.ldd + n0 + col0) * es;
           for (int r = lane >> 3; r < rows; r += 4, d += step) {
             const uint32_t src = stg + (uint32_t)r * 128u, key = (uint32_t)(r & 7);
             const uint32_t before = (16u - (uint32_t)(reinterpret_cast<uintptr_t>(d) & 15u)) & 15u;      // bytes in front of the first whole piece
@@ -607,6 +613,39 @@ bool encode(CUtensorMap* tm, CUtensorMapDataType type, const void* base, long lo
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Few tiles and a long K: K in up to eight parts, at least four stages each, whose sums in fp32 a second launch adds in order.
+// (us without and with: 16 x 1600 x 6400 13.4 and 8.3, 128 x 1600 x 6400 13.7 and 9.5, 256 x 256 x 8192 15.8 and 9.2, 100 x 500 x 2048 9.2
+// and 7.6, 128 x 1600 x 3200 8.9 and 8.6; parts of two or three stages lose: 16 x 768 x 1600 6.1 and 7.1.)
+int choose_splits(long long tiles, int kblocks, int slots) {
+  if (tiles * 2 > slots) return 1;
+  int n = (int)(slots / tiles);
+  if (n > kblocks / 4) n = kblocks / 4;
+  if (n > 8) n = 8;
+  return n < 2 ? 1 : n;
+}
+
+// D = alpha * the sum of the parts (and the matrices' scales), in order. A row of D a block row, four columns a thread.
+template <typename O>
+__global__ void __launch_bounds__(128) mx4_join_kernel(const float* parts, int splits, int M, int N, int np, long long part, O* D, long long ldd,
+                                                       long long batch_d, float alpha, const float* scale_a, const float* scale_b, int b_shared) {
+  const int z = blockIdx.y, bz = z / M, r = z - bz * M, c = 4 * ((int)blockIdx.x * 128 + (int)threadIdx.x);
+  pdl_wait();
+  if (c >= N) return;
+  const float* x = parts + (long long)z * np + c;
+  float4 sum = *reinterpret_cast<const float4*>(x);
+#pragma unroll 4
+  for (int k = 1; k < splits; ++k) {
+    const float4 y = *reinterpret_cast<const float4*>(x + k * part);
+    sum.x += y.x; sum.y += y.y; sum.z += y.z; sum.w += y.w;
+  }
+  if (scale_a) alpha *= scale_a[bz] * scale_b[b_shared ? 0 : bz];
+  const float v[4] = {alpha * sum.x, alpha * sum.y, alpha * sum.z, alpha * sum.w};
+  O* const d = D + bz * batch_d + (long long)r * ldd + c;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (c + j < N) d[j] = (O)v[j];
+}
+
 // Tile width: the one with the smallest modelled time in cycles. A stage takes the tensor pipe 2 cycles a column, at least what a step
 // of the issuing thread takes, at least its operand bytes at the 5500 bytes a cycle that L2 delivers to the chip; the read-out of a
 // tile overlaps the next tile's stages, except the last.
@@ -679,6 +718,24 @@ cudaError_t mx4_gemm_prepare() {
   return tc_limit<NVFP4, 1>();
 }
 
+Mx4Split mx4_gemm_split(int b, int M, int N, int K, int out_dtype, int num_sms) {
+  Mx4Split r = {1, 0};
+  if (M <= 8) return r;
+  Mx4Gemm g = {};
+  g.b = b; g.M = M; g.N = N; g.K = K; g.out_dtype = out_dtype;
+  const bool pair = M > 128;
+  const int bn = choose_width(g, pair, num_sms), kblocks = (mx4_width(K) + KB_ELEMENTS - 1) / KB_ELEMENTS;
+  const long long tiles = (long long)b * ((M + (pair ? 255 : 127)) / (pair ? 256 : 128)) * ((N + bn - 1) / bn);
+  r.splits = choose_splits(tiles, kblocks, pair ? num_sms / 2 : num_sms);
+  if (r.splits > 1) {
+    // (no part without a stage)
+    const int per = (kblocks + r.splits - 1) / r.splits;
+    r.splits = (kblocks + per - 1) / per;
+    r.work_bytes = (size_t)r.splits * b * M * ((N + 3) & ~3) * sizeof(float);
+  }
+  return r;
+}
+
 cudaError_t mx4_gemm_launch(const Mx4Gemm& g, cudaStream_t st, int* status, int num_sms, unsigned long long wait_ns, long long* launches) {
   if (g.M <= 8) {
     RowParams r;
@@ -689,6 +746,7 @@ cudaError_t mx4_gemm_launch(const Mx4Gemm& g, cudaStream_t st, int* status, int 
   }
   if (!encode_fn()) return cudaErrorNotSupported;
   const bool pair = g.M > 128;
+  const int slots = pair ? num_sms / 2 : num_sms;
   TcParams4 p;
   p.M = g.M; p.N = g.N; p.batch = g.b; p.b_shared = g.b_shared;
   p.BN = choose_width(g, pair, num_sms);
@@ -696,9 +754,12 @@ cudaError_t mx4_gemm_launch(const Mx4Gemm& g, cudaStream_t st, int* status, int 
   p.tiles_n = (g.N + p.BN - 1) / p.BN;
   const long long total = (long long)p.tiles_m * p.tiles_n * g.b;
   if (total > 0x3fffffff) return cudaErrorInvalidValue;
-  p.total_tiles = (int)total;
   const int width = mx4_width(g.K), atoms = g.fmt == MXFP4 ? 2 : 4;
   p.kblocks = (width + KB_ELEMENTS - 1) / KB_ELEMENTS;
+  const Mx4Split split = mx4_gemm_split(g.b, g.M, g.N, g.K, g.out_dtype, num_sms);
+  p.splits = g.work ? split.splits : 1;
+  p.kper = (p.kblocks + p.splits - 1) / p.splits;
+  p.total_tiles = (int)total * p.splits;
   p.ksteps_last = (width - (p.kblocks - 1) * KB_ELEMENTS + 63) / 64;
   const int nsb = p.BN <= 128 ? 1 : 2;
   p.overlap = 2 * p.BN > (int)scale_column(g.fmt) ? 2 * p.BN - (int)scale_column(g.fmt) : 0;
@@ -713,25 +774,39 @@ cudaError_t mx4_gemm_launch(const Mx4Gemm& g, cudaStream_t st, int* status, int 
   // kind::mxf4 / mxf4nvf4: e2m1 operands (1), both K-major; scales e8m0 (1) or e4m3 (0); M / 16 and N / 8 (added per tile)
   p.idesc = 1u << 7 | 1u << 10 | (g.fmt == MXFP4 ? 1u : 0u) << 23 | (pair ? 16u : 8u) << 24;
   p.out_f32 = g.out_dtype == F32;
-  p.D = g.D; p.ldd = g.ldd; p.batch_d = g.batch_d;
-  p.alpha = g.alpha; p.scale_a = g.A.scale; p.scale_b = g.B.scale;
+  const bool join = p.splits > 1;
+  const int np = (g.N + 3) & ~3, out_n = join ? np : g.N, out_b = p.splits * g.b;
+  p.out_f32 = join || g.out_dtype == F32;
+  if (join) { p.D = g.work; p.ldd = np; p.batch_d = (long long)g.M * np; }
+  else { p.D = g.D; p.ldd = g.ldd; p.batch_d = g.batch_d; }
+  p.alpha = join ? 1.f : g.alpha; p.scale_a = g.A.scale; p.scale_b = g.B.scale;
   p.status = status; p.wait_ns = wait_ns;
   const long long es = p.out_f32 ? 4 : 2;
   // (whole rows of 16-byte pieces: the copy engine writes the last piece in full, past a row that ends inside it)
-  p.store_tma = (reinterpret_cast<uintptr_t>(g.D) & 15u) == 0 && (g.N * es) % 16 == 0 && (g.ldd * es) % 16 == 0 && (g.b == 1 || (g.batch_d * es) % 16 == 0);
+  p.store_tma = (reinterpret_cast<uintptr_t>(p.D) & 15u) == 0 && (out_n * es) % 16 == 0 && (p.ldd * es) % 16 == 0 && (out_b == 1 || (p.batch_d * es) % 16 == 0);
   const int bb = g.b_shared ? 1 : g.b;
   bool ok = encode(&p.tmA, CU_TENSOR_MAP_DATA_TYPE_UINT8, g.A.codes, width / 2, g.M, g.b, width / 2, (long long)g.M * (width / 2), KB_BYTES, 128) &&
             encode(&p.tmB, CU_TENSOR_MAP_DATA_TYPE_UINT8, g.B.codes, width / 2, g.N, bb, width / 2, (long long)g.N * (width / 2), KB_BYTES, b_rows);
   p.sa = g.A.scales; p.sb = g.B.scales; p.rt_a = mx4_row_tiles(g.M); p.rt_b = mx4_row_tiles(g.N); p.kt = mx4_scale_tiles(g.K, g.fmt);
   if (ok && p.store_tma) {
-    const long long batch_bytes = g.b > 1 ? g.batch_d * es : g.ldd * es * g.M;
-    ok = encode(&p.tmD, p.out_f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, g.D, g.N, g.M, g.b, g.ldd * es, batch_bytes,
+    const long long batch_bytes = out_b > 1 ? p.batch_d * es : p.ldd * es * g.M;
+    ok = encode(&p.tmD, p.out_f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, p.D, out_n, g.M, out_b, p.ldd * es, batch_bytes,
                 p.out_f32 ? 32 : 64, 32);
   }
   if (!ok) return cudaErrorInvalidValue;
-  const int slots = pair ? num_sms / 2 : num_sms, runs = p.total_tiles < slots ? p.total_tiles : slots, grid = pair ? 2 * runs : runs;
+  const int runs = p.total_tiles < slots ? p.total_tiles : slots, grid = pair ? 2 * runs : runs;
   if (launches) ++*launches;
-  return g.fmt == MXFP4 ? tc_pick<MXFP4>(p, pair, nsb, grid, smem, st) : tc_pick<NVFP4>(p, pair, nsb, grid, smem, st);
+  const cudaError_t e = g.fmt == MXFP4 ? tc_pick<MXFP4>(p, pair, nsb, grid, smem, st) : tc_pick<NVFP4>(p, pair, nsb, grid, smem, st);
+  if (e != cudaSuccess || !join) return e;
+  if (launches) ++*launches;
+  const dim3 blocks((unsigned)((np / 4 + 127) / 128), (unsigned)(g.b * g.M));
+  const float* const sa = g.fmt == NVFP4 ? g.A.scale : nullptr;
+  const long long part = (long long)g.b * g.M * np;
+  if (g.out_dtype == F32)
+    return launch_kernel(mx4_join_kernel<float>, blocks, dim3(128), 0, st, (const float*)g.work, p.splits, g.M, g.N, np, part, (float*)g.D, g.ldd, g.batch_d,
+                         g.alpha, sa, g.B.scale, g.b_shared);
+  return launch_kernel(mx4_join_kernel<__nv_bfloat16>, blocks, dim3(128), 0, st, (const float*)g.work, p.splits, g.M, g.N, np, part, (__nv_bfloat16*)g.D, g.ldd,
+                       g.batch_d, g.alpha, sa, g.B.scale, g.b_shared);
 }
 
 }  // namespace defl

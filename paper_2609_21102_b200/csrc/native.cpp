@@ -263,8 +263,12 @@ PyObject* mx4_gemm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     if (M > 1) ld = out.stride(1);
   }
   if (b > 65535) return PyLong_FromLong(DEFL_ERR_RANK);
+  Tensor work;
+  const size_t room = defl_mx4_gemm_work_bytes(c, (int)b, side(M), side(N), side(K), type);
+  if (room) work = make({(int64_t)room}, at::kByte, device);
   use_stream(c, device);
-  const int rc = defl_mx4_gemm(c, &A, &B, (int)b, side(M), side(N), side(K), bb == 1, fmt, (float)alpha, out.data_ptr(), ld, out.stride(0), type);
+  const int rc = defl_mx4_gemm(c, &A, &B, (int)b, side(M), side(N), side(K), bb == 1, fmt, (float)alpha, out.data_ptr(), ld, out.stride(0), type,
+                               room ? work.data_ptr() : nullptr);
   return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(out);
   END_HANDLE_TH_ERRORS
 }

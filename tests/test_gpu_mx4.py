@@ -121,7 +121,8 @@ def _check(ctx, D, A, B, alpha=1.0, scale=1.0):
 ROWS = [(1, 1, 64, 32), (1, 1, 6400, 1600), (2, 3, 100, 1003), (1, 8, 700, 5000), (1, 5, 33, 9000), (1, 2, 1, 48), (3, 7, 1600, 96)]
 TILES = [(1, 9, 64, 32), (1, 128, 64, 64), (1, 128, 256, 512), (1, 100, 200, 1000), (2, 77, 6400, 1600), (1, 129, 1, 32), (1, 256, 64, 256),
          (1, 256, 256, 1024), (3, 333, 517, 1003), (1, 1024, 768, 768), (2, 2000, 1600, 640), (1, 4100, 6400, 32), (1, 4096, 4097, 300),
-         (1, 700, 192, 2048), (5, 260, 330, 80), (1, 16, 20000, 128), (1, 8192, 48, 64)]
+         (1, 700, 192, 2048), (5, 260, 330, 80), (1, 16, 20000, 128), (1, 8192, 48, 64),
+         (1, 128, 1600, 6400), (2, 40, 130, 5000), (1, 300, 100, 9001), (1, 9, 7, 2300)]          # the last four in parts along K
 
 
 @pytest.mark.gpu
@@ -151,6 +152,17 @@ def test_exact_sums(ctx, fmt, shape):
     (A, a), (B, c) = make(M), make(N)
     D = ctx.defl_mx4_gemm(A, B, out_dtype=F32)
     assert torch.equal(D.double(), a @ c.transpose(1, 2))
+
+
+@pytest.mark.gpu
+def test_which_products_go_in_parts(ctx):
+    from paper_2609_21102_b200 import binding
+    room = lambda *s: binding.lib().defl_mx4_gemm_work_bytes(ctx._h, *s, 0)  # noqa: E731
+    for b, M, N, K in TILES[-4:]:
+        parts = room(b, M, N, K) / (b * M * ((N + 3) // 4 * 4) * 4)
+        assert parts in (2, 3, 4, 5, 6, 7, 8)
+    for b, M, N, K in TILES[:-4] + ROWS:
+        assert room(b, M, N, K) == 0 or K >= 2048
 
 
 @pytest.mark.gpu
@@ -332,7 +344,8 @@ def test_refusals_and_sizes_without_a_device():
         binding._native().mx4_quantize(0, 0, None, "nvfp4", 1, binding.Mx4)
     assert L.defl_mx4_quantize(None, None, 0, 1, 1, 1, ctypes.c_int64(1), ctypes.c_int64(1), 0, None, None, None) == -1
     assert L.defl_mx4_dequantize(None, None, 1, 1, 1, 0, None, 0) == -1
-    assert L.defl_mx4_gemm(None, None, None, 1, 1, 1, 1, 0, 0, ctypes.c_float(1.0), None, ctypes.c_int64(1), ctypes.c_int64(1), 0) == -1
+    assert L.defl_mx4_gemm(None, None, None, 1, 1, 1, 1, 0, 0, ctypes.c_float(1.0), None, ctypes.c_int64(1), ctypes.c_int64(1), 0, None) == -1
+    assert L.defl_mx4_gemm_work_bytes(None, 1, 128, 64, 6400, 0) == 0
     for b, rows, cols in ((1, 1, 1), (2, 129, 33), (3, 128, 64), (1, 517, 1003)):
         for fmt, code in binding.MX4_FORMATS.items():
             # every block of a matrix has a byte in its tiles

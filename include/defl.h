@@ -393,7 +393,7 @@ int defl_grad_norm(defl_ctx* ctx, const defl_norm_tensor* tensors, int count, fl
  * Buffers of codes and scales start on 16-byte boundaries; sides are at most DEFL_MX4_MAX_SIDE. */
 #define DEFL_MXFP4 0
 #define DEFL_NVFP4 1
-#define DEFL_MX4_MAX_SIDE (1 << 24)
+#define DEFL_MX4_MAX_SIDE (1 << 23)
 typedef struct defl_mx4 {
   void* codes;
   void* scales;

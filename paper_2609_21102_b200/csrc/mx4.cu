@@ -158,6 +158,18 @@ __global__ void __launch_bounds__(Q_THREADS) mx4_quantize_kernel(const QuantPara
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
+  } else if (ES == 4) {
+    // rows that start anywhere: value by value, all on their way at once
+    const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem);
+    const int r0 = tid / TILE, c = tid % TILE;
+    const T* src = X + (long long)(row0 + r0) * p.ld + col0 + c;
+#pragma unroll 8
+    for (int i = 0; i < TILE * TILE / Q_THREADS; ++i, src += 2 * p.ld) {
+      const int r = r0 + 2 * i;
+      const bool on = row0 + r < p.rows && col0 + c < p.cols;
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(base + 4 * (row_word<T>(r) + c)), "l"(on ? src : X), "r"(on ? 4u : 0u) : "memory");
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   } else {
 #pragma unroll 16
     for (int i = 0; i < TILE * TILE / Q_THREADS; ++i) {
@@ -197,7 +209,7 @@ __global__ void __launch_bounds__(Q_THREADS) mx4_quantize_kernel(const QuantPara
     top = __reduce_max_sync(0xffffffffu, top);
     if (lane == 0) s_top[warp] = top;
   }
-  if (VEC) asm volatile("cp.async.wait_group 0;" ::: "memory");
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
   __syncthreads();
   if (FMT == NVFP4) {
     uint32_t top = 0;
@@ -385,16 +397,20 @@ __global__ void __launch_bounds__(Q_THREADS) mx4_amax_kernel(const void* Xv, lon
       if (sizeof(T) == 2 && !fine) top = __vmaxu2(top, m); else top = max(top, m);
     };
     const long long step = (long long)gridDim.x * Q_THREADS, u0 = (long long)blockIdx.x * Q_THREADS + threadIdx.x;
-    if (VEC && (ld == cols || rows == 1)) {
-      const long long n = (long long)rows * cols, nv = n / V;
-      const uint4* const P = reinterpret_cast<const uint4*>(X);
+    if (ld == cols || rows == 1) {
+      // one run of values: whole 16-byte pieces, and those before and after them
+      const long long n = (long long)rows * cols;
+      const long long skip = (long long)((16u - (uint32_t)(reinterpret_cast<uintptr_t>(X) & 15u)) & 15u) / (long long)sizeof(T), head = skip < n ? skip : n;
+      const long long nv = (n - head) / V, tail = head + nv * V;
+      const uint4* const P = reinterpret_cast<const uint4*>(X + head);
       long long u = u0;
       for (; u + 3 * step < nv; u += 4 * step) {
         const uint4 a = P[u], b = P[u + step], c = P[u + 2 * step], d = P[u + 3 * step];
         take(a); take(b); take(c); take(d);
       }
       for (; u < nv; u += step) take(P[u]);
-      if (u0 < n - nv * V) one(X[nv * V + u0]);
+      if (u0 < head) one(X[u0]);
+      if (u0 < n - tail) one(X[tail + u0]);
     } else {
       const long long per = VEC ? (cols + V - 1) / V : cols;
       // (row and column are carried along: the step is a fixed number of rows and columns)
@@ -430,7 +446,8 @@ __device__ __forceinline__ float2 e2m1x2(uint32_t two) {
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
-// A warp a row; eight values a lane and trip. Bound by HBM: half a byte in, 2 or 4 out.
+// A warp 1024 values of a row (256 where the rows do not start on 16-byte boundaries), all its loads on their way at once. Bound by HBM:
+// half a byte in, 2 or 4 out.
 template <int FMT, typename O>
 __global__ void __launch_bounds__(Q_THREADS) mx4_dequantize_kernel(Mx4View a, int b, int rows, int cols, O* out, int vec) {
   constexpr int BLK = FMT == MXFP4 ? 32 : 16;
@@ -443,31 +460,37 @@ __global__ void __launch_bounds__(Q_THREADS) mx4_dequantize_kernel(Mx4View a, in
   const uint8_t* const sc = a.scales + ((long long)bz * mx4_row_tiles(rows) + (r >> 7)) * kt * 512 + (r & 31) * 16 + ((r >> 5) & 3) * 4;
   const float whole = FMT == NVFP4 ? a.scale[bz] : 1.f;
   O* const dst = out + id * cols;
-#pragma unroll 4
-  for (int c8 = lane; c8 * 8 < cols; c8 += 32) {
-    const uint32_t q = codes[c8];
-    const int blk = c8 * 8 / BLK;
+  auto scale_of = [&](int blk) {
     const uint32_t byte = sc[(long long)(blk >> 2) * 512 + (blk & 3)];
-    float s;
-    if (FMT == MXFP4) s = byte == 255u ? __uint_as_float(0x7fffffffu) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
-    else s = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)byte, __NV_E4M3))) * whole;
+    if (FMT == MXFP4) return byte == 255u ? __uint_as_float(0x7fffffffu) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
+    return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)byte, __NV_E4M3))) * whole;
+  };
+  if (!vec) {
+    // rows that do not start on 16-byte boundaries: a value a lane, side by side
+    const int first = 256 * blockIdx.y, end = min(cols, first + 256);
+#pragma unroll 8
+    for (int c = first + lane; c < end; c += 32) {
+      const float2 f = e2m1x2(codes[c >> 3] >> (4 * (c & 6)));
+      dst[c] = (O)((c & 1 ? f.y : f.x) * scale_of(c / BLK));
+    }
+    return;
+  }
+  const int end = min(cols / 8, 128 * ((int)blockIdx.y + 1));
+#pragma unroll 4
+  for (int c8 = 128 * blockIdx.y + lane; c8 < end; c8 += 32) {
+    const uint32_t q = codes[c8];
+    const float s = scale_of(c8 * 8 / BLK);
     float v[8];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const float2 f = e2m1x2(q >> (8 * j));
       v[2 * j] = f.x * s; v[2 * j + 1] = f.y * s;
     }
-    if (vec) {
-      if (sizeof(O) == 2) {
-        *reinterpret_cast<uint4*>(dst + 8 * c8) = make_uint4(pack16x2(v[0], v[1], false), pack16x2(v[2], v[3], false), pack16x2(v[4], v[5], false), pack16x2(v[6], v[7], false));
-      } else {
-        reinterpret_cast<float4*>(dst + 8 * c8)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(dst + 8 * c8)[1] = make_float4(v[4], v[5], v[6], v[7]);
-      }
+    if (sizeof(O) == 2) {
+      *reinterpret_cast<uint4*>(dst + 8 * c8) = make_uint4(pack16x2(v[0], v[1], false), pack16x2(v[2], v[3], false), pack16x2(v[4], v[5], false), pack16x2(v[6], v[7], false));
     } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (8 * c8 + j < cols) dst[8 * c8 + j] = (O)v[j];
+      reinterpret_cast<float4*>(dst + 8 * c8)[0] = make_float4(v[0], v[1], v[2], v[3]);
+      reinterpret_cast<float4*>(dst + 8 * c8)[1] = make_float4(v[4], v[5], v[6], v[7]);
     }
   }
 }
@@ -581,7 +604,8 @@ int defl_mx4_dequantize(defl_ctx* c, const defl_mx4* a, int b, int rows, int col
   c->err[0] = 0;
   const Mx4View v = {(const uint8_t*)a->codes, (const uint8_t*)a->scales, a->scale};
   const int vec = on(out, 16) && cols % 8 == 0;
-  const dim3 g((unsigned)grid), t(Q_THREADS);
+  const int seg = vec ? 1024 : 256;
+  const dim3 g((unsigned)grid, (unsigned)((cols + seg - 1) / seg)), t(Q_THREADS);
   cudaError_t e;
   if (dtype == DEFL_BF16) {
     __nv_bfloat16* o = (__nv_bfloat16*)out;

@@ -163,6 +163,7 @@ PyObject* mx4_quantize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   TORCH_CHECK(PyType_Check(a[5]) && PyType_IsSubtype(reinterpret_cast<PyTypeObject*>(a[5]), &PyTuple_Type), "the last argument is a named tuple");
   defl_ctx* c = handle(a[0]);
   const int device = (int)PyLong_AsLong(a[1]), fmt = format_of(a[3]), which = (int)PyLong_AsLong(a[4]);
+  if (PyErr_Occurred()) throw python_error();
   const Tensor& X = tensor(a[2], "X");
   TORCH_CHECK_VALUE(X.dim() == 3 && X.is_cuda() && X.get_device() == device && (X.scalar_type() == at::kBFloat16 || X.scalar_type() == at::kFloat),
                     "X must be a bfloat16 or float32 tensor [b, rows, cols] on cuda:", device);

@@ -313,7 +313,7 @@ int defl_frobenius_norms_noalloc(const void* X, int dtype, int b, long long coun
  *   m <- beta1 m + (1 - beta1) g                 v <- beta2 v + (1 - beta2) g^2
  *   p <- (1 - lr * weight_decay) p - lr * (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
  * in fp32 whatever the types; t is the number of this step, counted from 1. The hyperparameters are doubles because 1 - 0.999f
- * is 1.3e-5 of itself away from 0.001. All pointers are device memory; the tensors of a list do not overlap one another
+ * is 1.3e-5 of itself away from 0.001 (an eps below 2^-126 counts as zero). All pointers are device memory; the tensors of a list do not overlap one another
  * (the same one twice is a race; the Python binding refuses it). A tensor with n = 0 or g = NULL is left alone.
  *
  * Moments in 8 bits (state_bits = 8): blocks of 256 consecutive elements of a tensor (the last one may be shorter), m and

@@ -111,14 +111,12 @@ __device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
   return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
 }
 
-// y >= 0 to a neighbouring e4m3 value, up with the probability of the part that is cut off: 16 random bits are added below
-// the three mantissa bits that stay, then the rest is cut. Below 2^-6, where e4m3 values are 2^-9 apart, the same is done
-// to y + 2^-6, whose spacing that is. (A block's largest y is 448 give or take two units of fp32: with those and all 16 bits
-// set it still does not reach the next spacing, so 448 stays 448.)
-__device__ __forceinline__ float e4m3_stochastic(float y, uint32_t bits16) {
-  const float low = y < 0.015625f ? 1.f : 0.f;
-  const uint32_t z = (__float_as_uint(fmaf(low, 0.015625f, y)) + (bits16 << 4)) & 0xFFF00000u;
-  return fmaf(low, -0.015625f, __uint_as_float(z));
+// y >= 0 to a neighbouring e4m3 value, up with the probability of the part that is cut off. y * 2^-120 has e4m3's exponents in fp32's
+// exponent field, and what is subnormal there is subnormal here: the bits above the 20 lowest are the code, in both ranges, and 16 random bits
+// are added below them. (A block's largest y is 448 give or take two units of fp32: with those and all 16 bits set it still does
+// not reach the next spacing, so 448 stays 448.) Returns the code at bit 20.
+__device__ __forceinline__ uint32_t e4m3_stochastic(float y, uint32_t bits16) {
+  return __float_as_uint(y * 7.52316384526264e-37f) + (bits16 << 4);
 }
 
 // fp32 to bf16 by 16 random bits, kept as fp32; Inf and NaN stay what they are
@@ -135,12 +133,17 @@ __device__ __forceinline__ void adam_one(const AdamHyper& h, const Scalars& s, f
   m = __fadd_rn(__fmul_rn(h.b1, m), __fmul_rn(h.ob1, g));
   v = __fadd_rn(__fmul_rn(h.b2, v), __fmul_rn(h.ob2, __fmul_rn(g, g)));
   root = sqrtf(v);
-  p = fmaf(-s.size, __fdividef(m, fmaf(root, s.rc2, h.eps)), p * s.keep);
+  // the reciprocal of a subnormal is taken as that of zero: a root is 0 or above 2^-75, so that only an eps below fp32's normal numbers
+  // counts as zero. (80M elements in 8 bits 242 -> 232 us against a division that minds the ends of the range.)
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(fmaf(root, s.rc2, h.eps)));
+  p = fmaf(-s.size, m * inv, p * s.keep);
 }
 
-__device__ __forceinline__ float max_nan(float a, float b) {     // a NaN is the largest
+// the largest magnitude of three; a NaN is the largest
+__device__ __forceinline__ float max_abs3(float a, float b, float c) {
   float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
 
@@ -168,7 +171,6 @@ __device__ __forceinline__ void adam_block(const AdamTensor& t, const AdamHyper&
                                            long long base, long long left, int lane) {
   P* const pp = reinterpret_cast<P*>(t.p) + base;
   const G* const gp = reinterpret_cast<const G*>(t.g) + base;
-  __nv_bfloat16* const cp = t.copy ? reinterpret_cast<__nv_bfloat16*>(t.copy) + base : nullptr;
   uint8_t* const m8 = reinterpret_cast<uint8_t*>(t.m) + base;
   uint8_t* const v8 = reinterpret_cast<uint8_t*>(t.v) + base;
   float* const m32 = reinterpret_cast<float*>(t.m) + base;
@@ -209,47 +211,63 @@ __device__ __forceinline__ void adam_block(const AdamTensor& t, const AdamHyper&
     adam_one(h, s, g[j], p[j], m[j], v[j], root);
     if (EIGHT) {
       v[j] = root;                                 // what is held
-      big_m = max_nan(big_m, fabsf(m[j]));
-      big_r = max_nan(big_r, root);
+      if (j & 1) {
+        big_m = max_abs3(big_m, m[j - 1], m[j]);
+        big_r = max_abs3(big_r, v[j - 1], v[j]);
+      }
     }
   }
   float inv_m = 0.f, inv_r = 0.f;
   if (EIGHT) {
     block_scales(big_m, big_r, lane, inv_m, inv_r, t.ms + block, t.vs + block);
   }
-  uint32_t cm[4], cv[4];
-  const unsigned long long lane_key = key ^ (unsigned long long)((base >> 1) + 4 * lane);
+  uint32_t cm[4], cv[4];                           // two codes each
+  const unsigned long long lane_key = key ^ (unsigned long long)((base >> 1) + (VEC ? 4 * lane : lane >> 1));
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     uint32_t bits[2] = {0, 0};
-    if (SR && VEC) {
-      const unsigned long long w = mix64(lane_key ^ (unsigned long long)j);        // (base / 2 + 4 lane is a multiple of four)
-      bits[0] = (uint32_t)w; bits[1] = (uint32_t)(w >> 32);
+    if (SR) {
+      if (VEC) {
+        const unsigned long long w = mix64(lane_key ^ (unsigned long long)j);      // (base / 2 + 4 lane is a multiple of four)
+        bits[0] = (uint32_t)w; bits[1] = (uint32_t)(w >> 32);
+      } else {
+        // two neighbouring lanes hold the halves of a pair: the even lane makes the word of their pair 2 j, the odd one of 2 j + 1
+        const int odd = lane & 1;
+        const unsigned long long w = mix64(lane_key ^ (unsigned long long)(16 * (2 * j + odd)));
+        const uint32_t mine = odd ? (uint32_t)(w >> 32) : (uint32_t)w;
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? (uint32_t)w : (uint32_t)(w >> 32), 1);
+        bits[0] = odd ? other : mine; bits[1] = odd ? mine : other;
+      }
     }
+    uint32_t qm[2], qv[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const int i = 2 * j + k;
-      if (SR && !VEC) {
-        const unsigned long long e = (unsigned long long)(base + lane + 32 * i), w = mix64(key ^ (e >> 1));
-        bits[k] = (e & 1) ? (uint32_t)(w >> 32) : (uint32_t)w;
-      }
       if (SR && sizeof(P) == 2) p[i] = bf16_stochastic(p[i], bits[k] >> 16);
       if (EIGHT) {
         const float a = fabsf(m[i]) * inv_m, b = v[i] * inv_r;
-        const float qa = SR ? e4m3_stochastic(a, bits[k] & 0xFFFFu) : a;
-        float qb = SR ? e4m3_stochastic(b, bits[k] >> 16) : b;
         // the root of what is not zero does not become zero: the moment beside it may be larger than its step's gradient,
-        // and would be divided by eps alone
-        if (b > 0.f) qb = fmaxf(qb, 0.001953125f);
-        m[i] = copysignf(qa, m[i]);
-        v[i] = qb;
+        // and would be divided by eps alone. (A root that is not zero is above 2^-75.)
+        if (SR) {
+          qm[k] = e4m3_stochastic(a, bits[k] & 0xFFFFu);
+          qv[k] = max(e4m3_stochastic(b, bits[k] >> 16), min(__float_as_uint(v[i]), 1u << 20));
+        } else {
+          m[i] = copysignf(a, m[i]);
+          v[i] = b > 0.f ? fmaxf(b, 0.001953125f) : b;
+        }
       }
     }
-    if (EIGHT) { cm[j] = to_e4m3x2(m[2 * j], m[2 * j + 1]); cv[j] = to_e4m3x2(v[2 * j], v[2 * j + 1]); }
+    if (EIGHT && SR) {
+      cm[j] = (qm[0] >> 20 | (qm[1] >> 20) << 8) | (__byte_perm(__float_as_uint(m[2 * j]), __float_as_uint(m[2 * j + 1]), 0x73) & 0x8080u);
+      cv[j] = qv[0] >> 20 | (qv[1] >> 20) << 8;
+    } else if (EIGHT) {
+      cm[j] = to_e4m3x2(m[2 * j], m[2 * j + 1]);
+      cv[j] = to_e4m3x2(v[2 * j], v[2 * j + 1]);
+    }
   }
   if (VEC) {
     store8(pp + 8 * lane, p);
-    if (cp) store8(cp + 8 * lane, p);
+    if (t.copy) store8(reinterpret_cast<__nv_bfloat16*>(t.copy) + base + 8 * lane, p);
     if (EIGHT) {
       reinterpret_cast<uint2*>(m8)[lane] = make_uint2(cm[0] | (cm[1] << 16), cm[2] | (cm[3] << 16));
       reinterpret_cast<uint2*>(v8)[lane] = make_uint2(cv[0] | (cv[1] << 16), cv[2] | (cv[3] << 16));
@@ -263,7 +281,7 @@ __device__ __forceinline__ void adam_block(const AdamTensor& t, const AdamHyper&
       const int e = lane + 32 * j;
       if (e < left) {
         pp[e] = (P)p[j];
-        if (cp) cp[e] = __float2bfloat16_rn(p[j]);
+        if (t.copy) reinterpret_cast<__nv_bfloat16*>(t.copy)[base + e] = __float2bfloat16_rn(p[j]);
         if (EIGHT) {
           m8[e] = (uint8_t)(cm[j >> 1] >> (8 * (j & 1)));
           v8[e] = (uint8_t)(cv[j >> 1] >> (8 * (j & 1)));
@@ -277,7 +295,10 @@ __device__ __forceinline__ void adam_block(const AdamTensor& t, const AdamHyper&
 }
 
 // Bytes an element with fp32 weights and bf16 gradients: 26 with 32-bit moments, 14.1 with 8-bit ones; what HBM can bring of
-// that in a second leaves 150 and 77 instructions an element.
+// that in a second leaves 150 and 77 instructions an element. 80M elements on a B200: 312 us with 32-bit moments (6.7 TB/s: bound by HBM), with
+// 8-bit ones 194 to nearest and 230 with random bits, which are bound by the issue of instructions (about 90 an element, 84 % of the slots
+// taken): the generator's two 64-bit products and shifts take 28 us of that, the exact square root 14. Two blocks a trip take registers that spill
+// (276), three CTAs an SM leave too little to hide (255).
 template <typename P, typename G, bool EIGHT, bool SR, int CAP>
 __global__ void __launch_bounds__(OPT_THREADS, 4) adamw_kernel(const __grid_constant__ AdamTable<CAP> tb) {
   __shared__ Scalars sc;

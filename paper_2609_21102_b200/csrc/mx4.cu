@@ -95,12 +95,21 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t big, float whole, flo
 // The quotient value / s correctly rounded, so that the ties between two codes, which values of few bits often hit, are ties.
 // SHORT (values of 8 bits): value * r.hi is exact and value * r.lo brings the sum to 2^-39 of the quotient, far nearer than any
 // quotient that is not a tie comes to one. Else the rounded product and one correction by its exact remainder (Markstein 1990).
+// Two values at a time: one instruction multiplies both (8192 x 6400 bf16 to nvfp4 60.5 -> 58.3 us).
 template <int FMT, bool SHORT>
-__device__ __forceinline__ float scaled(float x, const BlockScale& q) {
-  if (FMT == MXFP4) return x * q.r;
-  if (SHORT) return fmaf(x, q.lo, x * q.r);
-  const float a = x * q.r;
-  return fmaf(fmaf(-a, q.s, x), q.r, a);
+__device__ __forceinline__ void scaled2(float x0, float x1, const BlockScale& q, float* v) {
+  if (FMT == MXFP4) {
+    v[0] = x0 * q.r;
+    v[1] = x1 * q.r;
+  } else if (SHORT) {
+    asm("{\n\t.reg .b64 x, r, l, a;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 r, {%4, %4};\n\tmov.b64 l, {%5, %5};\n\t"
+        "mul.rn.f32x2 a, x, r;\n\tfma.rn.f32x2 a, x, l, a;\n\tmov.b64 {%0, %1}, a;\n\t}"
+        : "=f"(v[0]), "=f"(v[1]) : "f"(x0), "f"(x1), "f"(q.r), "f"(q.lo));
+  } else {
+    asm("{\n\t.reg .b64 x, r, n, a, e;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 r, {%4, %4};\n\tmov.b64 n, {%5, %5};\n\t"
+        "mul.rn.f32x2 a, x, r;\n\tfma.rn.f32x2 e, a, n, x;\n\tfma.rn.f32x2 a, e, r, a;\n\tmov.b64 {%0, %1}, a;\n\t}"
+        : "=f"(v[0]), "=f"(v[1]) : "f"(x0), "f"(x1), "f"(q.r), "f"(-q.s));
+  }
 }
 
 // the larger magnitudes of two pairs of bf16 (signs mean nothing), NaN above all
@@ -135,7 +144,9 @@ __global__ void __launch_bounds__(Q_THREADS) mx4_quantize_kernel(const QuantPara
   uint32_t* const words = reinterpret_cast<uint32_t*>(smem);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int bz = blockIdx.y;
-  const int tr = (int)(blockIdx.x / (unsigned)p.tiles_c), tc = (int)(blockIdx.x - (unsigned)tr * (unsigned)p.tiles_c);
+  // (nvfp4: the last tiles first, since the search for the largest magnitude has just left them in L2: 8192 x 6400 in bf16 64 -> 60 us)
+  const unsigned int tile = FMT == NVFP4 ? gridDim.x - 1u - blockIdx.x : blockIdx.x;
+  const int tr = (int)(tile / (unsigned)p.tiles_c), tc = (int)(tile - (unsigned)tr * (unsigned)p.tiles_c);
   const int row0 = tr * TILE, col0 = tc * TILE;
   const T* const X = reinterpret_cast<const T*>(p.X) + (long long)bz * p.batch_stride;
   pdl_wait();
@@ -281,14 +292,13 @@ __global__ void __launch_bounds__(Q_THREADS) mx4_quantize_kernel(const QuantPara
             if (FMT == MXFP4) {
               widen(x, (uint16_t)(__float_as_uint(c.r) >> 16), v[2 * j], v[2 * j + 1]);
             } else {
-              v[2 * j] = scaled<FMT, true>(__uint_as_float(x << 16), c);
-              v[2 * j + 1] = scaled<FMT, true>(__uint_as_float(x & 0xffff0000u), c);
+              scaled2<FMT, true>(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u), c, v + 2 * j);
             }
           }
           codes[k] = e2m1x8(v);
         } else {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] = scaled<FMT, false>(__uint_as_float(w[8 * k + j]), c);
+          for (int j = 0; j < 8; j += 2) scaled2<FMT, false>(__uint_as_float(w[8 * k + j]), __uint_as_float(w[8 * k + j + 1]), c, v + j);
           const uint32_t x = e2m1x8(v);
           codes[k] = odd ? __byte_perm(x, x, 0x1032) : x;
         }
@@ -342,7 +352,8 @@ __global__ void __launch_bounds__(Q_THREADS) mx4_quantize_kernel(const QuantPara
                 widen(x, (uint16_t)(__float_as_uint(q.r) >> 16), lo, hi);
                 v[j] = k == 0 ? lo : hi;
               } else {
-                v[j] = scaled<FMT, ES == 2>(__uint_as_float(ES == 4 ? x : k == 0 ? x << 16 : x & 0xffff0000u), q);
+                v[j] = __uint_as_float(ES == 4 ? x : k == 0 ? x << 16 : x & 0xffff0000u);
+                if (j & 1) scaled2<FMT, ES == 2>(v[j - 1], v[j], q, v + j - 1);
               }
             }
             codes[(BLK / 8) * h + o] = e2m1x8(v);

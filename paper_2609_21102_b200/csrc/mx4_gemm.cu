@@ -56,6 +56,20 @@ struct TcParams4 {
   int* status; unsigned long long wait_ns;
 };
 
+// alpha and the matrices' scales in one factor, and `pre`, 1 except where that factor leaves the middle of fp32's range: two matrices of values
+// near 1e25 have 2^150 between them, and a sum of zero times that is zero. (A sum that is not zero is between 2^-20 and 2^46 in magnitude, so
+// that a factor cut at fp32's largest number still makes it infinite.)
+__device__ __forceinline__ float output_factor(float alpha, float scale_a, float scale_b, float& pre) {
+  const float both = scale_a * scale_b, f = alpha * both;
+  pre = 1.f;
+  if (fabsf(both) > 0x1p-100f && fabsf(both) < 0x1p100f && (alpha == 0.f || (fabsf(f) > 0x1p-100f && fabsf(f) < 0x1p100f))) return f;
+  const double exact = (double)alpha * (double)scale_a * (double)scale_b, size = fabs(exact);
+  if (!(size < 1e300)) return (float)exact;          // a scale or alpha that is not finite
+  pre = size > 1.0 ? 0x1p64f : 0x1p-64f;
+  const double rest = exact / (double)pre;
+  return (float)(rest > 3.4028234663852886e38 ? 3.4028234663852886e38 : rest < -3.4028234663852886e38 ? -3.4028234663852886e38 : rest);
+}
+
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
@@ -333,8 +347,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
     for (int tile = tile0, it = 0; tile < p.total_tiles; tile += tile_step, ++it) {
       const Tile4 t = tile_of<PAIR>(p, tile);
       const uint32_t acc = (uint32_t)it & 1u, use = ((uint32_t)it >> 1) & 1u;
-      float alpha = p.alpha;
-      if (FMT == NVFP4 && p.splits == 1) alpha *= p.scale_a[t.bz] * p.scale_b[p.b_shared ? 0 : t.bz];
+      float alpha = p.alpha, pre = 1.f;
+      if (FMT == NVFP4 && p.splits == 1) alpha = output_factor(alpha, p.scale_a[t.bz], p.scale_b[p.b_shared ? 0 : t.bz], pre);
       const int out_z = t.ks * p.batch + t.bz;
       if (!mbar_wait(smem_u32(&acc_full_bar[acc]), use, &abort_flag, p.status, p.wait_ns)) break;
       tc_fence_after();
@@ -368,6 +382,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
         if (ovl_now || last) tell(ovl_now, last);
         told = told || ovl_now;
         if (!active) continue;
+        if (FMT == NVFP4 && pre != 1.f) {
+#pragma unroll
+          for (int j = 0; j < 64; ++j)
+            if (j < 32 || !p.out_f32) r[j] = __float_as_uint(pre * __uint_as_float(r[j]));
+        }
         // the last store has read the buffer
         asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
         __syncwarp();
@@ -575,11 +594,12 @@ __global__ void __launch_bounds__(ROW_THREADS) mx4_row_kernel(const RowParams p)
     }
   }
   if (row_ok && at0 == 0) {
-    float alpha = p.alpha;
-    if (FMT == NVFP4) alpha *= p.A.scale[bz] * p.B.scale[bb];
+    float alpha = p.alpha, pre = 1.f;
+    if (FMT == NVFP4) alpha = output_factor(alpha, p.A.scale[bz], p.B.scale[bb], pre);
 #pragma unroll
     for (int t = 0; t < T; ++t)
       if (t < p.M) {
+        sum[t] *= pre;
         const long long at = (long long)bz * p.batch_d + (long long)t * p.ldd + n;
         if (p.out_f32) reinterpret_cast<float*>(p.D)[at] = alpha * sum[t];
         else reinterpret_cast<__nv_bfloat16*>(p.D)[at] = __float2bfloat16_rn(alpha * sum[t]);
@@ -638,8 +658,9 @@ __global__ void __launch_bounds__(128) mx4_join_kernel(const float* parts, int s
     const float4 y = *reinterpret_cast<const float4*>(x + k * part);
     sum.x += y.x; sum.y += y.y; sum.z += y.z; sum.w += y.w;
   }
-  if (scale_a) alpha *= scale_a[bz] * scale_b[b_shared ? 0 : bz];
-  const float v[4] = {alpha * sum.x, alpha * sum.y, alpha * sum.z, alpha * sum.w};
+  float pre = 1.f;
+  if (scale_a) alpha = output_factor(alpha, scale_a[bz], scale_b[b_shared ? 0 : bz], pre);
+  const float v[4] = {alpha * (pre * sum.x), alpha * (pre * sum.y), alpha * (pre * sum.z), alpha * (pre * sum.w)};
   O* const d = D + bz * batch_d + (long long)r * ldd + c;
 #pragma unroll
   for (int j = 0; j < 4; ++j)

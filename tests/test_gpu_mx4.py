@@ -194,6 +194,29 @@ def test_any_matrix_scale(ctx, M):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("shape", [(4, 200, 64), (64, 200, 320), (300, 200, 64), (16, 40, 4096)])
+def test_scales_that_leave_fp32_together(ctx, fmt, shape):
+    """Values near 2^83 on both sides: a sum of zeros is zero. nvfp4 forms its sums before the matrices' scales meet them: what is
+    not zero is infinite with its sign, and values near 2^-93 and 2^-67 with an alpha of 2^100 give ordinary numbers. (mxfp4 has no
+    scale of a matrix: there each product leaves fp32 by itself.) Factors are powers of two, so that the codes stay the same."""
+    M, N, K = shape
+    a, w = _rand((1, M, K), 13, F32, 0.0).cuda(), _rand((1, N, K), 14, F32, 0.0).cuda()
+    a[0, 1], a[0, 2, 1:], w[0, 5] = 0.0, 0.0, 0.0
+    a[0, 2, 0], w[0, :, 0] = 3.0, 0.0
+    D = ctx.defl_mx4_gemm(ctx.defl_mx4_quantize(a * 2.0 ** 83, fmt), ctx.defl_mx4_quantize(w * 2.0 ** 83, fmt), out_dtype=F32)
+    zero = torch.zeros_like(D, dtype=torch.bool)
+    zero[0, 1], zero[0, 2], zero[0, :, 5] = True, True, True
+    assert torch.all(D[zero] == 0)
+    if fmt == "nvfp4":
+        plain = ctx.defl_mx4_gemm(ctx.defl_mx4_quantize(a, fmt), ctx.defl_mx4_quantize(w, fmt), out_dtype=F32)
+        large = plain != 0
+        assert torch.all(D[large] == plain[large] * float("inf"))
+        A, B = ctx.defl_mx4_quantize(a * 2.0 ** -93, fmt), ctx.defl_mx4_quantize(w * 2.0 ** -67, fmt)
+        _check(ctx, ctx.defl_mx4_gemm(A, B, out_dtype=F32, alpha=2.0 ** 100), A, B, 2.0 ** 100)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("M", [8, 64, 300])
 def test_not_finite(ctx, fmt, M):
     """A block that is not finite makes NaN of its row (A) or column (B) of the product and of nothing else."""

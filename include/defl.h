@@ -419,7 +419,7 @@ int defl_mx4_quantize(defl_ctx* ctx, const void* X, int dtype, int b, int rows, 
 int defl_mx4_dequantize(defl_ctx* ctx, const defl_mx4* a, int b, int rows, int cols, int fmt, void* out, int dtype);
 
 /* D [b, M, N] = alpha A B^T with A [b, M, K] and B [b, N, K], or one B for all (b_shared != 0), of the same format; D row-major with row
- * stride ldd >= N and a batch stride of its own, DEFL_BF16 or DEFL_F32, apart from A and B. Products are exact, sums are fp32, one rounding to bf16.
+ * stride ldd >= N and a batch stride of at least (M - 1) ldd + N, DEFL_BF16 or DEFL_F32, apart from A and B. Products are exact, sums are fp32, one rounding to bf16.
  * Up to eight rows of A (single tokens) the weights stream through integer products, else the tensor cores take the
  * scales with the codes (tcgen05 block-scaled products). A device-side wait that runs out is reported by
  * defl_device_wait_status. Errors as defl_mx4_quantize. */

@@ -209,7 +209,8 @@ class Mx4(NamedTuple):
 class AdamWGroup:
     """The tensors of defl_adamw_step, checked once: parameters (float32 or bfloat16), first and second moments of the same
     sizes, all float32 or, in 8 bits, float8_e4m3fn with float32 scales [ceil(n / 256)] (the second moment is held as its
-    root); optional bfloat16 copies of the parameters. The group keeps the tensors alive; no two of them may overlap."""
+    root); optional bfloat16 copies of the parameters. The group keeps the tensors' memory alive; no two of them may overlap.
+    A parameter that has been given other memory since (p.data = ..., .to(...)) is refused: it needs a new group."""
 
     def __init__(self, params, exp_avg, exp_avg_sq, avg_scale=None, root_scale=None, copies=None):
         self.params, self.exp_avg, self.exp_avg_sq = list(params), list(exp_avg), list(exp_avg_sq)
@@ -221,6 +222,9 @@ class AdamWGroup:
         lists = (self.params, self.exp_avg, self.exp_avg_sq, self.avg_scale, self.root_scale, self.copies)
         if any(len(x) != count for x in lists):
             raise ValueError("the lists of an AdamWGroup must have one entry per parameter")
+        # what the table points to stays, whatever becomes of the tensors
+        self._params = tuple(self.params)
+        self._memory = [[t.detach() for t in x if t is not None] for x in lists]
         self.device = self.params[0].device if count else None
         self.sizes = [p.numel() for p in self.params]
         self.table = np.zeros(count, dtype=_ADAMW_TENSOR)
@@ -501,7 +505,7 @@ class Context:
         tensor [1]; grad_scale: defl_grad_norm's result, whose factor multiplies the gradients (0: the step is left out)."""
         if group.device is not None and group.device != self.device:
             raise ValueError("the group's tensors are on %s, the context is on %s" % (group.device, self.device))
-        self._check(_native().adamw_step(self._handle, self._index, group.address, group.count, grads, lr, step, betas[0], betas[1], eps,
+        self._check(_native().adamw_step(self._handle, self._index, group.address, group._params, grads, lr, step, betas[0], betas[1], eps,
                                          weight_decay, grad_scale, stochastic, seed))
 
     def _scalar(self, t, dtype, count, what):

@@ -38,7 +38,7 @@ void use_stream(defl_ctx* c, int device) { defl_set_stream(c, c10::cuda::getCurr
 
 struct Sequence {
   PyObject* fast;
-  explicit Sequence(PyObject* o) : fast(PySequence_Fast(o, "gradients must be a list or a tuple")) { if (!fast) throw python_error(); }
+  explicit Sequence(PyObject* o) : fast(PySequence_Fast(o, "must be a list or a tuple")) { if (!fast) throw python_error(); }
   ~Sequence() { Py_DECREF(fast); }
   Py_ssize_t size() const { return PySequence_Fast_GET_SIZE(fast); }
   PyObject* operator[](Py_ssize_t i) const { return PySequence_Fast_GET_ITEM(fast, i); }
@@ -56,15 +56,15 @@ bool gradient(PyObject* o, Py_ssize_t i, int device, const void** x, int64_t* n,
   return true;
 }
 
-// adamw_step(handle, device, table address, count, grads, lr, step, beta1, beta2, eps, weight_decay, grad_scale, stochastic, seed) -> code
+// adamw_step(handle, device, table address, params, grads, lr, step, beta1, beta2, eps, weight_decay, grad_scale, stochastic, seed) -> code
 PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
   TORCH_CHECK(nargs == 14, "adamw_step takes 14 arguments");
   defl_ctx* c = handle(a[0]);
   const int device = (int)PyLong_AsLong(a[1]);
   defl_adamw_tensor* table = reinterpret_cast<defl_adamw_tensor*>(PyLong_AsVoidPtr(a[2]));
-  const long count = PyLong_AsLong(a[3]);
-  const Sequence grads(a[4]);
+  const Sequence params(a[3]), grads(a[4]);
+  const Py_ssize_t count = params.size();
   TORCH_CHECK_VALUE(grads.size() == count, grads.size(), " gradients for ", count, " parameters");
   defl_adamw_opts o = {};
   if (THPVariable_Check(a[5])) o.lr_dev = (const float*)scalar(a[5], device, at::kFloat, 1, "lr"); else o.lr = PyFloat_AsDouble(a[5]);
@@ -74,8 +74,10 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   o.stochastic = PyObject_IsTrue(a[12]);
   o.seed = PyLong_AsUnsignedLongLongMask(a[13]);
   if (PyErr_Occurred()) throw python_error();
-  for (long i = 0; i < count; ++i) {
+  for (Py_ssize_t i = 0; i < count; ++i) {
     int64_t n = 0;
+    const Tensor& p = tensor(params[i], "a parameter");
+    TORCH_CHECK_VALUE(p.data_ptr() == table[i].p && p.numel() == table[i].n, "parameter ", i, " has other memory than when its AdamWGroup was made");
     table[i].g = nullptr;
     if (!gradient(grads[i], i, device, &table[i].g, &n, &table[i].g_dtype)) continue;
     TORCH_CHECK_VALUE(n == table[i].n, "gradient ", i, " has ", n, " elements, its parameter ", table[i].n);

@@ -302,6 +302,37 @@ def test_muon_takes_the_factor(ctx):
 
 
 @pytest.mark.gpu
+def test_a_parameter_that_has_moved(ctx):
+    """A group made before a parameter was given other memory is refused, and what it points to is still there."""
+    from paper_2609_21102_b200 import binding
+    p = torch.nn.Parameter(torch.ones(1000, device="cuda"))
+    group = binding.AdamWGroup([p], [torch.zeros(1000, device="cuda")], [torch.zeros(1000, device="cuda")])
+    g = torch.ones(1000, device="cuda")
+    ctx.defl_adamw_step(group, [g], LR, 1)
+    old = group._memory[0][0]
+    assert old.data_ptr() == p.data_ptr() and torch.all(p != 1)
+    p.data = p.data.clone()
+    kept = p.detach().clone()
+    with pytest.raises(ValueError):
+        ctx.defl_adamw_step(group, [g], LR, 2)
+    assert torch.equal(p.detach(), kept) and torch.equal(old, kept)
+
+
+@pytest.mark.gpu
+def test_smallest_eps(ctx):
+    """An eps below fp32's normal numbers is zero; where both moments are, the quotient is then NaN, as 0 / 0 is."""
+    from paper_2609_21102_b200 import binding
+    for eps, dead in ((0.0, True), (1e-40, True), (2e-38, False)):
+        p, m, v = (torch.full((512,), x, device="cuda") for x in (1.0, 0.0, 0.0))
+        g = torch.zeros(512, device="cuda")
+        g[::2] = 0.5
+        ctx.defl_adamw_step(binding.AdamWGroup([p], [m], [v]), [g], LR, 1, eps=eps, weight_decay=0.0)
+        # the first step is lr in the gradient's direction: a reciprocal, two products and a difference
+        assert float((p[::2].double() - (1 - LR)).abs().max()) <= 8 * 2.0 ** -24
+        assert torch.isnan(p[1::2]).all() if dead else torch.all(p[1::2] == 1)
+
+
+@pytest.mark.gpu
 def test_refusals(ctx):
     from paper_2609_21102_b200 import binding
     f = lambda n, dtype=F32: torch.zeros(n, dtype=dtype, device="cuda")  # noqa: E731
@@ -373,4 +404,4 @@ def test_refusals_without_a_device():
     with pytest.raises(TypeError):
         binding._native().grad_norm(0, 0, [3], 1.0, None, None)
     with pytest.raises(ValueError):
-        binding._native().adamw_step(0, 0, 0, 1, [], 1e-3, 1, 0.9, 0.999, 1e-8, 0.0, None, False, 0)
+        binding._native().adamw_step(0, 0, 0, [torch.zeros(3)], [], 1e-3, 1, 0.9, 0.999, 1e-8, 0.0, None, False, 0)

@@ -11,9 +11,9 @@
 // Tensor memory: 512 columns = two accumulators and four sets of scales (24 columns each, nvfp4 48). Two accumulators of 256 columns
 // leave no room for that, so they overlap (by 96 and 192 columns); the read-out takes those first and says so, and the next tile's
 // products wait for that much only. (Copies run on meanwhile, and products are twice as fast as copies.)
-// What bounds it: at 5 PFLOP/s (8192 x 8192 x 8192: mxfp4 5.4 in 202 us, nvfp4 4.9 in 224) the operands of a 256 x 256 tile (64 + 6 KB,
-// nvfp4 + 12 KB, per 256 values of K and pair) come at what L2 delivers to the whole chip, 5500 to 6000 bytes a cycle, and the clock falls
-// under the power cap; short K is bound by the read-out and by writing D (8192 x 6400 x 1600 to bf16: 48 and 53 us, D alone 16 of HBM).
+// What bounds it: what L2 delivers to the whole chip, 11 TB/s (5500 to 6000 bytes a cycle at 1.9 GHz). 8192 x 8192 x 8192 takes that for
+// operands alone, 64 + 6 KB (nvfp4 + 12) for a 256 x 256 tile and 256 values of K: 207 us in mxfp4, 5.3 PFLOP/s, 224 in nvfp4. 8192 x 6400 x
+// 1600 to bf16, 47 and 52 us, moves 530 and 556 MB through L2, 105 of them D.
 //
 // mx4_row_kernel, for up to eight rows of A: the weights are read once at memory speed, each code becomes two bytes by table
 // lookup (prmt), four products at a time are integer dot products (dp4a), a block's sum meets its scales in fp32.

@@ -483,7 +483,8 @@ __device__ __forceinline__ float2 e2m1x2(uint32_t two) {
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
-// A warp 1024 values of a row (256 where the rows do not start on 16-byte boundaries), all its loads on their way at once. Bound by HBM:
+constexpr int SEG = 64;                    // 32-byte pieces of a row of the result that a warp takes
+// A warp 2 KB of a row of the result (256 values where the rows do not start on 16-byte boundaries), all its loads on their way at once. Bound by HBM:
 // half a byte in, 2 or 4 out.
 template <int FMT, typename O>
 __global__ void __launch_bounds__(Q_THREADS) mx4_dequantize_kernel(Mx4View a, int b, int rows, int cols, O* out, int vec) {
@@ -512,22 +513,29 @@ __global__ void __launch_bounds__(Q_THREADS) mx4_dequantize_kernel(Mx4View a, in
     }
     return;
   }
-  const int end = min(cols / 8, 128 * ((int)blockIdx.y + 1));
-#pragma unroll 4
-  for (int c8 = 128 * blockIdx.y + lane; c8 < end; c8 += 32) {
-    const uint32_t q = codes[c8];
-    const float s = scale_of(c8 * 8 / BLK);
-    float v[8];
+  // a lane writes 32 bytes, a whole sector, in one store where rows start on such boundaries (8192 x 6400 to bf16 32 -> 25 us, to fp32
+  // 58 -> 42, against 16 bytes at a time; one or four pieces a lane in place of two gain nothing)
+  constexpr int PER = 32 / (int)sizeof(O);
+  const int end = min((cols + PER - 1) / PER, SEG * ((int)blockIdx.y + 1));
+#pragma unroll 2
+  for (int u = SEG * blockIdx.y + lane; u < end; u += 32) {
+    uint32_t q[PER / 8];
+    if (PER == 16) { const uint2 two = reinterpret_cast<const uint2*>(codes)[u]; q[0] = two.x; q[PER / 8 - 1] = two.y; } else { q[0] = codes[u]; }
+    const float s = scale_of(u * PER / BLK);
+    uint32_t w[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float2 f = e2m1x2(q >> (8 * j));
-      v[2 * j] = f.x * s; v[2 * j + 1] = f.y * s;
+    for (int j = 0; j < PER / 2; ++j) {
+      const float2 f = e2m1x2(q[j / 4] >> (8 * (j & 3)));
+      if (PER == 16) { w[j & 7] = pack16x2(f.x * s, f.y * s, false); }
+      else { w[(2 * j) & 7] = __float_as_uint(f.x * s); w[(2 * j + 1) & 7] = __float_as_uint(f.y * s); }
     }
-    if (sizeof(O) == 2) {
-      *reinterpret_cast<uint4*>(dst + 8 * c8) = make_uint4(pack16x2(v[0], v[1], false), pack16x2(v[2], v[3], false), pack16x2(v[4], v[5], false), pack16x2(v[6], v[7], false));
+    O* const d = dst + (long long)PER * u;
+    if (vec == 2) {
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                   ::"l"(d), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
     } else {
-      reinterpret_cast<float4*>(dst + 8 * c8)[0] = make_float4(v[0], v[1], v[2], v[3]);
-      reinterpret_cast<float4*>(dst + 8 * c8)[1] = make_float4(v[4], v[5], v[6], v[7]);
+      reinterpret_cast<uint4*>(d)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+      if (PER == 8 || 16 * u + 8 < cols) reinterpret_cast<uint4*>(d)[1] = make_uint4(w[4], w[5], w[6], w[7]);
     }
   }
 }
@@ -640,8 +648,9 @@ int defl_mx4_dequantize(defl_ctx* c, const defl_mx4* a, int b, int rows, int col
   DeviceScope scope(c->device);
   c->err[0] = 0;
   const Mx4View v = {(const uint8_t*)a->codes, (const uint8_t*)a->scales, a->scale};
-  const int vec = on(out, 16) && cols % 8 == 0;
-  const int seg = vec ? 1024 : 256;
+  // 0: value by value, 1: 16-byte stores, 2: 32-byte stores
+  const int es = (int)dtype_size(dtype), vec = on(out, 32) && (long long)cols * es % 32 == 0 ? 2 : on(out, 16) && cols % 8 == 0 ? 1 : 0;
+  const int seg = vec ? 32 / es * SEG : 256;
   const dim3 g((unsigned)grid, (unsigned)((cols + seg - 1) / seg)), t(Q_THREADS);
   cudaError_t e;
   if (dtype == DEFL_BF16) {

@@ -104,6 +104,35 @@ def test_quantise_where_it_can_go_wrong(ctx, fmt, dtype):
         _same(qt, P.transpose(0, 2, 1), fmt)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("offset", [0, 16, 4])
+@pytest.mark.parametrize("shape", [(2, 33, 40), (1, 5, 1000), (1, 3, 4112), (2, 9, 1003)])
+def test_dequantise_into_any_place(ctx, fmt, dtype, offset, shape):
+    """Results that start on 32, 16 or 4 bytes, rows that do and do not: the values of the codes, and nothing beside them."""
+    import ctypes
+    from paper_2609_21102_b200 import binding
+    q = ctx.defl_mx4_quantize(_rand(shape, 15, F32).cuda(), fmt)
+    n, es = int(np.prod(shape)), 2 if dtype == BF16 else 4
+    buf = torch.full((n * es + 96,), 0x5a, dtype=torch.uint8, device="cuda")
+    ref = (ctypes.c_void_p * 3)(q.codes.data_ptr(), q.scales.data_ptr(), q.scale.data_ptr() if q.scale is not None else None)
+    torch.cuda.synchronize()
+    rc = binding.lib().defl_mx4_dequantize(ctypes.c_void_p(ctx._handle), ref, *shape, binding.MX4_FORMATS[fmt], ctypes.c_void_p(buf.data_ptr() + 32 + offset),
+                                           binding.BF16 if dtype == BF16 else binding.F32)
+    torch.cuda.synchronize()
+    assert rc == 0
+    host = buf.cpu().numpy()
+    assert np.all(host[:32 + offset] == 0x5a) and np.all(host[32 + offset + n * es:] == 0x5a)
+    got = torch.from_numpy(host[32 + offset:32 + offset + n * es].copy()).view(dtype).double().reshape(shape).numpy()
+    codes = q.codes.cpu().numpy()
+    for i in range(shape[0]):
+        index = np.stack([codes[i] & 15, codes[i] >> 4], axis=2).reshape(shape[1], -1).astype(np.int64)
+        value = np.array([0, .5, 1, 1.5, 2, 3, 4, 6])[index & 7] * np.where(index >= 8, -1.0, 1.0)
+        scale = mx4.decode_scale(q.plain_scales()[i].cpu().numpy().astype(np.int64), fmt, float(q.scale[i]) if q.scale is not None else 1.0)
+        assert np.array_equal(got[i], (value * np.repeat(scale, mx4.BLOCK[fmt], axis=1))[:, :shape[2]])
+
+
 def _mx(ctx, shape, seed, fmt, dtype=F32, spread=1.0):
     return ctx.defl_mx4_quantize(_rand(shape, seed, dtype, spread).cuda(), fmt)
 

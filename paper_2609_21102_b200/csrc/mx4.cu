@@ -435,17 +435,29 @@ __global__ void __launch_bounds__(Q_THREADS) mx4_amax_kernel(const void* Xv, lon
     };
     const long long step = (long long)gridDim.x * Q_THREADS, u0 = (long long)blockIdx.x * Q_THREADS + threadIdx.x;
     if (ld == cols || rows == 1) {
-      // one run of values: whole 16-byte pieces, and those before and after them
+      // one run of values: whole 32-byte pieces (16-byte ones: 8192 x 1600 quantised in 16.9 us, not 16.0), and those before and after them
+      constexpr int V2 = 2 * V;
       const long long n = (long long)rows * cols;
-      const long long skip = (long long)((16u - (uint32_t)(reinterpret_cast<uintptr_t>(X) & 15u)) & 15u) / (long long)sizeof(T), head = skip < n ? skip : n;
-      const long long nv = (n - head) / V, tail = head + nv * V;
-      const uint4* const P = reinterpret_cast<const uint4*>(X + head);
+      const long long skip = (long long)((32u - (uint32_t)(reinterpret_cast<uintptr_t>(X) & 31u)) & 31u) / (long long)sizeof(T), head = skip < n ? skip : n;
+      const long long nv = (n - head) / V2, tail = head + nv * V2;
+      const T* const P = X + head;
       long long u = u0;
+      auto load = [&](long long at, uint4& a, uint4& b) {
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "l"(P + at * V2));
+      };
       for (; u + 3 * step < nv; u += 4 * step) {
-        const uint4 a = P[u], b = P[u + step], c = P[u + 2 * step], d = P[u + 3 * step];
-        take(a); take(b); take(c); take(d);
+        uint4 q[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) load(u + k * step, q[2 * k], q[2 * k + 1]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) take(q[k]);
       }
-      for (; u < nv; u += step) take(P[u]);
+      for (; u < nv; u += step) {
+        uint4 x, y;
+        load(u, x, y);
+        take(x); take(y);
+      }
       if (u0 < head) one(X[u0]);
       if (u0 < n - tail) one(X[tail + u0]);
     } else {

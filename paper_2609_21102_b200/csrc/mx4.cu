@@ -133,7 +133,7 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t b
 }
 
 // Reads 2 or 4 bytes a value and writes half a byte and 1/32 or 1/16 a direction: HBM leaves some fifteen instructions a value, which mxfp4
-// stays below (8192 x 6400 bf16 in both directions 28 us, 5.8 TB/s) and nvfp4, about twenty, does not (39 us behind 19 of the search for
+// stays below (8192 x 6400 bf16 in both directions 28 us, 5.8 TB/s) and nvfp4, about twenty, does not (39 us behind 18 of the search for
 // the largest magnitude). The tile goes through shared memory once; both passes read it from there.
 template <typename T, int FMT, bool VEC>
 __global__ void __launch_bounds__(Q_THREADS) mx4_quantize_kernel(const QuantParams p) {

@@ -683,7 +683,7 @@ int choose_width(const Mx4Gemm& g, bool pair, int num_sms) {
     const double live = (tiles < slots ? tiles : slots) * (pair ? 2 : 1);
     double step = 2.0 * bn;
     if (step < 300.0) step = 300.0;
-    const double bytes = (128.0 + (pair ? bn / 2 : bn)) * KB_BYTES + 3072.0;
+    const double bytes = (128.0 + (pair ? bn / 2 : bn)) * KB_BYTES + 6.0 * 512.0;      // (and the scales)
     if (step < bytes * live / 5500.0) step = bytes * live / 5500.0;
     const double out = 1000.0 + bn * (g.out_dtype == F32 ? 16.0 : 10.0);
     const double t = (waves - 1.0) * (kb * step > out ? kb * step : out) + kb * step + out;

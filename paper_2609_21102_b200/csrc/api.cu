@@ -335,6 +335,7 @@ int defl_create(defl_ctx** out, int device) {
   c->knobs.paired_steps = getenv("DEFL_NO_PAIRED_STEPS") ? 0 : 1;
   c->knobs.lanczos_form = getenv("DEFL_LANCZOS_FORM") ? atoi(getenv("DEFL_LANCZOS_FORM")) : 0;
   c->knobs.lanczos_hold = getenv("DEFL_LANCZOS_HOLD") ? 1 : 0;
+  c->knobs.mx4_hold = getenv("DEFL_MX4_HOLD") ? 1 : 0;
   cudaDeviceGetAttribute(&c->num_sms, cudaDevAttrMultiProcessorCount, device);
   int ok = gemm_tc_prepare() == cudaSuccess && panel_prepare() == cudaSuccess && psd_prepare() == cudaSuccess &&
            mx4_quantize_prepare() == cudaSuccess && mx4_gemm_prepare() == cudaSuccess ? 1 : 0;

@@ -27,6 +27,6 @@ struct Mx4Split { int splits; size_t work_bytes; };
 Mx4Split mx4_gemm_split(int b, int M, int N, int K, int out_dtype, int num_sms);
 cudaError_t mx4_gemm_prepare();
 cudaError_t mx4_quantize_prepare();
-cudaError_t mx4_gemm_launch(const Mx4Gemm& g, cudaStream_t st, int* status, int num_sms, unsigned long long wait_ns, long long* launches);
+cudaError_t mx4_gemm_launch(const Mx4Gemm& g, cudaStream_t st, int* status, int num_sms, unsigned long long wait_ns, bool hold, long long* launches);
 
 }  // namespace defl

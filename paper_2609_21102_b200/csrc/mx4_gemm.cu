@@ -55,6 +55,7 @@ struct TcParams4 {
   void* D; long long ldd, batch_d;
   float alpha; const float* scale_a; const float* scale_b;
   int* status; unsigned long long wait_ns;
+  int hold;                                        // test hook: the codes of every CTA's first stage are neither announced nor copied
 };
 
 // alpha and the matrices' scales in one factor, and `pre`, 1 except where that factor leaves the middle of fp32's range: two matrices of values
@@ -209,8 +210,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
         if (lane == 0) ok = mbar_wait(empty0 + 8u * stage, phase ^ 1u, &abort_flag, p.status, p.wait_ns) ? 1 : 0;
         ok = __shfl_sync(0xffffffffu, ok, 0);
         if (!ok) { live = false; break; }
-        if (lane == 0 && rank == 0) mbar_expect_tx(full0 + 8u * stage, tx);
-        if (lane < 2) {
+        const bool held = p.hold && tile == tile0 && kb == t.k0;
+        if (lane == 0 && rank == 0 && !held) mbar_expect_tx(full0 + 8u * stage, tx);
+        if (lane < 2 && !held) {
           const uint32_t dst = smem_base + stage * p.stage_bytes + off;
           if (PAIR) tma_load_3d_pair(dst, tm, full0_sig + 8u * stage, kb * KB_BYTES, c1, c2);
           else tma_load_3d(dst, tm, full0 + 8u * stage, kb * KB_BYTES, c1, c2);
@@ -351,7 +353,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
       float alpha = p.alpha, pre = 1.f;
       if (FMT == NVFP4 && p.splits == 1) alpha = output_factor(alpha, p.scale_a[t.bz], p.scale_b[p.b_shared ? 0 : t.bz], pre);
       const int out_z = t.ks * p.batch + t.bz;
-      if (!mbar_wait(smem_u32(&acc_full_bar[acc]), use, &abort_flag, p.status, p.wait_ns)) break;
+      // (the warp goes on or gives up as one: what follows needs all its lanes)
+      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&acc_full_bar[acc]), use, &abort_flag, p.status, p.wait_ns))) break;
       tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (acc ? acc1 : 0u);
       const int row0 = t.tm * TILE_M + (int)rank * 128 + q * 32, n0 = t.tn * p.BN;
@@ -758,7 +761,7 @@ Mx4Split mx4_gemm_split(int b, int M, int N, int K, int out_dtype, int num_sms) 
   return r;
 }
 
-cudaError_t mx4_gemm_launch(const Mx4Gemm& g, cudaStream_t st, int* status, int num_sms, unsigned long long wait_ns, long long* launches) {
+cudaError_t mx4_gemm_launch(const Mx4Gemm& g, cudaStream_t st, int* status, int num_sms, unsigned long long wait_ns, bool hold, long long* launches) {
   if (g.M <= 8) {
     RowParams r;
     r.A = g.A; r.B = g.B; r.M = g.M; r.N = g.N; r.K = g.K; r.b_shared = g.b_shared;
@@ -802,7 +805,7 @@ cudaError_t mx4_gemm_launch(const Mx4Gemm& g, cudaStream_t st, int* status, int 
   if (join) { p.D = g.work; p.ldd = np; p.batch_d = (long long)g.M * np; }
   else { p.D = g.D; p.ldd = g.ldd; p.batch_d = g.batch_d; }
   p.alpha = join ? 1.f : g.alpha; p.scale_a = g.A.scale; p.scale_b = g.B.scale;
-  p.status = status; p.wait_ns = wait_ns;
+  p.status = status; p.wait_ns = wait_ns; p.hold = hold;
   const long long es = p.out_f32 ? 4 : 2;
   // (whole rows of 16-byte pieces: the copy engine writes the last piece in full, past a row that ends inside it)
   p.store_tma = (reinterpret_cast<uintptr_t>(p.D) & 15u) == 0 && (out_n * es) % 16 == 0 && (p.ldd * es) % 16 == 0 && (out_b == 1 || (p.batch_d * es) % 16 == 0);

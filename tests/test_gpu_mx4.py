@@ -406,3 +406,29 @@ def test_refusals_and_sizes_without_a_device():
             assert L.defl_mx4_scales_bytes(b, rows, cols, code) == b * mx4.tiles(byte).size
     assert L.defl_mx4_codes_bytes(0, 1, 1) == 0 and L.defl_mx4_scales_bytes(1, 1, 1, 7) == 0 and L.defl_mx4_work_bytes(0) == 0
     assert L.defl_mx4_work_bytes(1) == 592 * 4 and L.defl_mx4_work_bytes(1000) == 4000
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("shape", [(1, 64, 64, 64), (1, 300, 256, 512), (2, 700, 600, 4000), (1, 9, 7, 2300)])
+def test_bounded_wait_runs_out_and_is_reported(monkeypatch, ctx, fmt, shape):
+    """A wait that nothing satisfies ends in a status bit and a normal return: the codes of every CTA's first stage are neither announced
+    nor copied, with the limit at 2 ms (one CTA a tile, pairs, several tiles a pair, parts along K). What was asked for has landed long
+    before the waits give up; the word stays until it is cleared and the context stays usable."""
+    from paper_2609_21102_b200 import binding
+    b, M, N, K = shape
+    A, B = _mx(ctx, (b, M, K), 31, fmt), _mx(ctx, (b, N, K), 32, fmt)
+    few = A._replace(codes=A.codes[:, :8].contiguous(), scales=A.scales[:, :1].contiguous(), rows=8)
+    torch.cuda.synchronize()
+    monkeypatch.setenv("DEFL_MX4_HOLD", "1")
+    monkeypatch.setenv("DEFL_TC_WAIT_MS", "2")
+    held = binding.Context(0)
+    assert held.defl_device_wait_status() == 0
+    held.defl_mx4_gemm(A, B)
+    assert held.defl_device_wait_status(clear=False) == binding.ST_DEVICE_WAIT
+    assert held.defl_device_wait_status() == binding.ST_DEVICE_WAIT and held.defl_device_wait_status() == 0
+    _check(held, held.defl_mx4_gemm(few, B, out_dtype=F32), few, B)            # (up to eight rows nothing waits)
+    assert held.defl_device_wait_status() == 0
+    held.close()
+    _check(ctx, ctx.defl_mx4_gemm(A, B, out_dtype=F32), A, B)
+    assert ctx.defl_device_wait_status() == 0

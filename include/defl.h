@@ -458,12 +458,14 @@ int defl_get_stage_ms_sum(defl_ctx* ctx, float* ms, int cap, int ncalls);
 /* Number of kernels the library launched on this context since creation. */
 long long defl_launch_count(defl_ctx* ctx);
 
-/* The tensor engine's wait word of this context: every device-side wait of its kernels (on a copy, on a free
- * pipeline stage, on an accumulator) is bounded; one that runs out sets DEFL_ST_DEVICE_WAIT in this word, the kernel
- * stops waiting, lets its copies land, frees its tensor memory and returns. defl_polar_batched, defl_psd_project
- * and the calls built on them clear the word when they start and fold it into defl_info.status when they end; this
- * call is for the others (defl_debug_gemm). It synchronises the context's stream, returns the word (>= 0, or a
- * negative DEFL_ERR_*), and clears it when `clear` is non-zero. No counterpart in the paper. */
+/* The wait words of this context: every device-side wait of the tensor-core kernels (on a copy, on a free pipeline
+ * stage, on an accumulator) is bounded; one that runs out sets DEFL_ST_DEVICE_WAIT in a word, the kernel stops
+ * waiting, lets its copies land, frees its tensor memory and returns. The tensor engine has one word:
+ * defl_polar_batched, defl_psd_project and the calls built on them clear it when they start and fold it into
+ * defl_info.status when they end. defl_mx4_gemm has a word of its own, which no other call clears: what a training step's
+ * backward pass raised is still there after the optimizer. This call is for defl_debug_gemm and defl_mx4_gemm: it synchronises
+ * the context's stream, returns both words together (>= 0, or a negative DEFL_ERR_*), and clears them when `clear` is
+ * non-zero. No counterpart in the paper. */
 int defl_device_wait_status(defl_ctx* ctx, int clear);
 
 const char* defl_status_string(int code);

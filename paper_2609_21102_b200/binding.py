@@ -591,7 +591,8 @@ class Context:
         return int(lib().defl_launch_count(self._h))
 
     def defl_device_wait_status(self, clear=True):
-        """The tensor engine's wait word (DEFL_ST_DEVICE_WAIT if a bounded device-side wait ran out); synchronises."""
+        """The context's wait words together (DEFL_ST_DEVICE_WAIT if a bounded wait of the tensor engine or of a 4-bit product ran out);
+        synchronises its stream."""
         rc = lib().defl_device_wait_status(self._h, int(bool(clear)))
         if rc < 0:
             self._check(rc)

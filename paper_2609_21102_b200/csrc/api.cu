@@ -339,8 +339,8 @@ int defl_create(defl_ctx** out, int device) {
   cudaDeviceGetAttribute(&c->num_sms, cudaDevAttrMultiProcessorCount, device);
   int ok = gemm_tc_prepare() == cudaSuccess && panel_prepare() == cudaSuccess && psd_prepare() == cudaSuccess &&
            mx4_quantize_prepare() == cudaSuccess && mx4_gemm_prepare() == cudaSuccess ? 1 : 0;
-  if (ok && cudaMalloc(&c->wait_status, 2 * sizeof(int)) != cudaSuccess) ok = 0;      // status word, tile counter
-  if (ok) cudaMemset(c->wait_status, 0, 2 * sizeof(int));
+  if (ok && cudaMalloc(&c->wait_status, WAIT_WORDS * sizeof(int)) != cudaSuccess) ok = 0;
+  if (ok) cudaMemset(c->wait_status, 0, WAIT_WORDS * sizeof(int));
   if (ok) {
     // identity tile of the tensor engine's identity segment (X0 = (G - head) / rho adds G in the accumulator)
     const size_t ib = 256 * 256 * sizeof(__nv_bfloat16);
@@ -447,12 +447,13 @@ long long defl_launch_count(defl_ctx* c) { return c ? c->launches : 0; }
 int defl_device_wait_status(defl_ctx* c, int clear) {
   if (!c) return DEFL_ERR_ARG;
   cudaSetDevice(c->device);
-  int word = 0;
+  int words[WAIT_WORDS] = {};
   if (ctx_fail(c, cudaStreamSynchronize(c->stream), "synchronize") ||
-      ctx_fail(c, cudaMemcpy(&word, c->wait_status, sizeof(int), cudaMemcpyDeviceToHost), "read status word"))
+      ctx_fail(c, cudaMemcpy(words, c->wait_status, sizeof(words), cudaMemcpyDeviceToHost), "read status word"))
     return DEFL_ERR_CUDA;
-  if (clear && word && ctx_fail(c, cudaMemset(c->wait_status, 0, sizeof(int)), "clear status word")) return DEFL_ERR_CUDA;
-  return word;
+  for (int i : {0, WAIT_MX4})
+    if (clear && words[i] && ctx_fail(c, cudaMemset(c->wait_status + i, 0, sizeof(int)), "clear status word")) return DEFL_ERR_CUDA;
+  return words[0] | words[WAIT_MX4];
 }
 
 // Window sizes from the paper's ratios (host arithmetic only).

@@ -22,7 +22,8 @@ struct defl_ctx {
   cudaEvent_t chunk_in[DEFL_HOST_MAX_CHUNKS], chunk_done[DEFL_HOST_MAX_CHUNKS];
   int copy_ready;                           // streams and events above exist
   int* wait_status;      // device words: [0] the tensor engine ORs DEFL_ST_DEVICE_WAIT into it (cleared at the start of
-                         // every polar / PSD call), [1] its tile counter
+                         // every polar / PSD call), [1] its tile counter, [WAIT_MX4] the 4-bit products' own (a call of another
+                         // kind, on this stream or another, neither clears nor takes it)
   defl::TcKnobs tc_knobs;        // tuning overrides, read from the environment when the context was created
   // DEFL_NO_TRANSPOSED_APPLY, DEFL_HOST_CHUNKS, DEFL_JACOBI_SWEEPS, DEFL_NO_PAIRED_STEPS, DEFL_LANCZOS_FORM, DEFL_LANCZOS_HOLD, DEFL_MX4_HOLD
   struct { int transposed_apply, host_chunks, jacobi_sweeps, paired_steps, lanczos_form, lanczos_hold, mx4_hold; } knobs;
@@ -39,6 +40,7 @@ struct defl_ctx {
 };
 
 namespace defl {
+constexpr int WAIT_MX4 = 2, WAIT_WORDS = 3;
 size_t align_up(size_t x, size_t a);
 bool ctx_fail(defl_ctx* c, cudaError_t e, const char* where);
 int ctx_reserve(defl_ctx* c, size_t bytes);

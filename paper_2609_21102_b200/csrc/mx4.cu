@@ -700,7 +700,7 @@ int defl_mx4_gemm(defl_ctx* c, const defl_mx4* A, const defl_mx4* B, int b, int 
   g.b = b; g.M = M; g.N = N; g.K = K; g.fmt = fmt; g.b_shared = b_shared != 0;
   g.D = D; g.ldd = ldd; g.batch_d = batch_stride; g.out_dtype = out_dtype; g.alpha = alpha; g.work = work;
   const unsigned long long wait_ns = (unsigned long long)(c->tc_knobs.wait_ms > 0 ? c->tc_knobs.wait_ms : 2000) * 1000000ull;
-  if (ctx_fail(c, mx4_gemm_launch(g, c->stream, c->wait_status, c->num_sms, wait_ns, c->knobs.mx4_hold != 0, &c->launches), "mx4 gemm")) return DEFL_ERR_CUDA;
+  if (ctx_fail(c, mx4_gemm_launch(g, c->stream, c->wait_status + WAIT_MX4, c->num_sms, wait_ns, c->knobs.mx4_hold != 0, &c->launches), "mx4 gemm")) return DEFL_ERR_CUDA;
   return DEFL_OK;
 }
 

@@ -432,3 +432,24 @@ def test_bounded_wait_runs_out_and_is_reported(monkeypatch, ctx, fmt, shape):
     held.close()
     _check(ctx, ctx.defl_mx4_gemm(A, B, out_dtype=F32), A, B)
     assert ctx.defl_device_wait_status() == 0
+
+
+@pytest.mark.gpu
+def test_wait_that_ran_out_is_not_lost_in_a_later_call(monkeypatch):
+    """The order of a training step on one context: a 4-bit product whose wait runs out, then calls that clear and report a wait word of
+    their own. The product's bit is still there, and is nobody else's."""
+    from paper_2609_21102_b200 import binding
+    monkeypatch.setenv("DEFL_MX4_HOLD", "1")
+    monkeypatch.setenv("DEFL_TC_WAIT_MS", "50")
+    held = binding.Context(0)
+    A, B = _mx(held, (1, 300, 256), 33, "nvfp4"), _mx(held, (1, 128, 256), 34, "nvfp4")
+    G = torch.tensor(np.random.default_rng(35).standard_normal((2, 128, 256))).float().cuda()
+    sched = [list(binding.MUON_QUINTIC)] * 5
+    held.defl_mx4_gemm(A, B)
+    _, info = held.defl_polar_batched(G.bfloat16(), 4, 4, 1, sched, seed=1, want_info=True)
+    held.defl_muon_step_batched(G.clone(), G.clone(), G, 0.02, 0.9, 4, 4, 1, sched)
+    held.defl_psd_project((G[0, :, :128] + G[0, :, :128].T).contiguous(), 0, torch.eye(128, device="cuda")[:, :4].contiguous(), [list(binding.CLASSICAL_QUINTIC)] * 3)
+    assert info["status"].cpu().tolist() == [0, 0]
+    assert held.defl_device_wait_status(clear=False) == binding.ST_DEVICE_WAIT
+    assert held.defl_device_wait_status() == binding.ST_DEVICE_WAIT and held.defl_device_wait_status() == 0
+    held.close()

@@ -7,6 +7,8 @@
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAStream.h>
 #include <c10/core/ScalarTypeToTypeMeta.h>
+#include <map>
+#include <mutex>
 #include "../../include/defl.h"
 
 namespace {
@@ -36,12 +38,29 @@ Tensor make(at::IntArrayRef shape, ScalarType type, int device) {
 }
 void use_stream(defl_ctx* c, int device) { defl_set_stream(c, c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream()); }
 
+// Python's lock is given up where the library allocates and launches: a launch waits while its stream's queue is full, and what the stream waits for
+// may be another thread of the program. Nothing of Python's is touched meanwhile. Setting the stream and the call belong together, so calls
+// on one context take turns.
+std::mutex& lock_of(defl_ctx* c) {
+  static std::mutex all;
+  static auto* each = new std::map<defl_ctx*, std::mutex>;
+  const std::lock_guard<std::mutex> one(all);
+  return (*each)[c];
+}
+struct Unlocked {
+  PyThreadState* const state;
+  std::unique_lock<std::mutex> turn;
+  explicit Unlocked(defl_ctx* c) : state(PyEval_SaveThread()), turn(lock_of(c)) {}
+  ~Unlocked() { turn.unlock(); PyEval_RestoreThread(state); }
+};
+
+// A tuple: another thread may change a list while this one is without Python's lock.
 struct Sequence {
-  PyObject* fast;
-  explicit Sequence(PyObject* o) : fast(PySequence_Fast(o, "must be a list or a tuple")) { if (!fast) throw python_error(); }
-  ~Sequence() { Py_DECREF(fast); }
-  Py_ssize_t size() const { return PySequence_Fast_GET_SIZE(fast); }
-  PyObject* operator[](Py_ssize_t i) const { return PySequence_Fast_GET_ITEM(fast, i); }
+  PyObject* items;
+  explicit Sequence(PyObject* o) : items(PySequence_Tuple(o)) { if (!items) throw python_error(); }
+  ~Sequence() { Py_DECREF(items); }
+  Py_ssize_t size() const { return PyTuple_GET_SIZE(items); }
+  PyObject* operator[](Py_ssize_t i) const { return PyTuple_GET_ITEM(items, i); }
 };
 // address and type of gradient i after its checks; false for None
 bool gradient(PyObject* o, Py_ssize_t i, int device, const void** x, int64_t* n, int* type) {
@@ -62,7 +81,7 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   TORCH_CHECK(nargs == 14, "adamw_step takes 14 arguments");
   defl_ctx* c = handle(a[0]);
   const int device = (int)PyLong_AsLong(a[1]);
-  defl_adamw_tensor* table = reinterpret_cast<defl_adamw_tensor*>(PyLong_AsVoidPtr(a[2]));
+  const defl_adamw_tensor* held = reinterpret_cast<const defl_adamw_tensor*>(PyLong_AsVoidPtr(a[2]));
   const Sequence params(a[3]), grads(a[4]);
   const Py_ssize_t count = params.size();
   TORCH_CHECK_VALUE(grads.size() == count, grads.size(), " gradients for ", count, " parameters");
@@ -74,6 +93,8 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   o.stochastic = PyObject_IsTrue(a[12]);
   o.seed = PyLong_AsUnsignedLongLongMask(a[13]);
   if (PyErr_Occurred()) throw python_error();
+  // (a copy for this call, with its gradients: the group's table is shared by all)
+  std::vector<defl_adamw_tensor> table(held, held + count);
   for (Py_ssize_t i = 0; i < count; ++i) {
     int64_t n = 0;
     const Tensor& p = tensor(params[i], "a parameter");
@@ -82,8 +103,13 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     if (!gradient(grads[i], i, device, &table[i].g, &n, &table[i].g_dtype)) continue;
     TORCH_CHECK_VALUE(n == table[i].n, "gradient ", i, " has ", n, " elements, its parameter ", table[i].n);
   }
-  use_stream(c, device);
-  return PyLong_FromLong(defl_adamw_step(c, table, (int)count, &o));
+  int rc;
+  {
+    const Unlocked unlocked(c);
+    use_stream(c, device);
+    rc = defl_adamw_step(c, table.data(), (int)count, &o);
+  }
+  return PyLong_FromLong(rc);
   END_HANDLE_TH_ERRORS
 }
 
@@ -104,10 +130,15 @@ PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     if (gradient(grads[i], i, device, &t.x, &t.n, &t.dtype)) ++count;
   }
   Tensor out;
-  if (is_none(a[4])) out = make({2}, at::kFloat, device); else { scalar(a[4], device, at::kFloat, 2, "out"); out = THPVariable_Unpack(a[4]); }
-  const Tensor work = make({(int64_t)defl_grad_norm_work_bytes(count)}, at::kByte, device);
-  use_stream(c, device);
-  const int rc = defl_grad_norm(c, table.data(), count, max_norm, out.data_ptr<float>(), step, work.data_ptr());
+  if (!is_none(a[4])) { scalar(a[4], device, at::kFloat, 2, "out"); out = THPVariable_Unpack(a[4]); }
+  int rc;
+  {
+    const Unlocked unlocked(c);
+    if (!out.defined()) out = make({2}, at::kFloat, device);
+    const Tensor work = make({(int64_t)defl_grad_norm_work_bytes(count)}, at::kByte, device);
+    use_stream(c, device);
+    rc = defl_grad_norm(c, table.data(), count, max_norm, out.data_ptr<float>(), step, work.data_ptr());
+  }
   return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(out);
   END_HANDLE_TH_ERRORS
 }
@@ -173,25 +204,29 @@ PyObject* mx4_quantize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   int64_t rows = m, cols = n, sr = X.stride(1), sc = X.stride(2);
   if (b <= 0 || rows <= 0 || cols <= 0) return PyLong_FromLong(DEFL_ERR_ARG);
   if (b > 65535 || rows > DEFL_MX4_MAX_SIDE || cols > DEFL_MX4_MAX_SIDE) return PyLong_FromLong(DEFL_ERR_RANK);
-  std::optional<Made> by_rows, by_cols;
-  if (which & 1) by_rows.emplace(b, rows, cols, fmt, device);
-  if (which & 2) by_cols.emplace(b, cols, rows, fmt, device);
-  defl_mx4* r = by_rows ? &by_rows->ref : nullptr;
-  defl_mx4* t = by_cols ? &by_cols->ref : nullptr;
-  if (cols > 1 && sc != 1) {
-    // the same matrices, seen from the other side
+  // the same matrices, seen from the other side
+  const bool turned = cols > 1 && sc != 1;
+  if (turned) {
     TORCH_CHECK_VALUE(rows == 1 || sr == 1, "one of X's last two dimensions must be contiguous");
     std::swap(rows, cols);
-    std::swap(r, t);
     sr = sc;
   }
   if (rows == 1) sr = cols;
   TORCH_CHECK_VALUE(sr >= cols, "X's rows overlap");
-  Tensor work;
-  if (fmt == DEFL_NVFP4 && rows * cols > 32768) work = make({(int64_t)defl_mx4_work_bytes((int)b)}, at::kByte, device);
-  use_stream(c, device);
-  const int rc = defl_mx4_quantize(c, X.data_ptr(), code_of(X.scalar_type()), (int)b, (int)rows, (int)cols, sr, X.stride(0), fmt, r, t,
-                                   work.defined() ? work.data_ptr() : nullptr);
+  std::optional<Made> by_rows, by_cols;
+  int rc;
+  {
+    const Unlocked unlocked(c);
+    if (which & 1) by_rows.emplace(b, m, n, fmt, device);
+    if (which & 2) by_cols.emplace(b, n, m, fmt, device);
+    const defl_mx4 *r = by_rows ? &by_rows->ref : nullptr, *t = by_cols ? &by_cols->ref : nullptr;
+    if (turned) std::swap(r, t);
+    Tensor work;
+    if (fmt == DEFL_NVFP4 && rows * cols > 32768) work = make({(int64_t)defl_mx4_work_bytes((int)b)}, at::kByte, device);
+    use_stream(c, device);
+    rc = defl_mx4_quantize(c, X.data_ptr(), code_of(X.scalar_type()), (int)b, (int)rows, (int)cols, sr, X.stride(0), fmt, r, t,
+                           work.defined() ? work.data_ptr() : nullptr);
+  }
   if (rc) return PyLong_FromLong(rc);
   if (which == 3) {
     PyObject* first = by_rows->object(a[5], a[3], m, n);
@@ -232,9 +267,14 @@ PyObject* mx4_dequantize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   if (PyErr_Occurred()) throw python_error();
   const defl_mx4 q = reference(a + 2, fmt, rows, cols, device, &b, "q");
   if (b > INT_MAX || (type != DEFL_BF16 && type != DEFL_F32)) return PyLong_FromLong(DEFL_ERR_ARG);
-  Tensor out = make({b, rows, cols}, type == DEFL_BF16 ? at::kBFloat16 : at::kFloat, device);
-  use_stream(c, device);
-  const int rc = defl_mx4_dequantize(c, &q, (int)b, side(rows), side(cols), fmt, out.data_ptr(), type);
+  Tensor out;
+  int rc;
+  {
+    const Unlocked unlocked(c);
+    out = make({b, rows, cols}, type == DEFL_BF16 ? at::kBFloat16 : at::kFloat, device);
+    use_stream(c, device);
+    rc = defl_mx4_dequantize(c, &q, (int)b, side(rows), side(cols), fmt, out.data_ptr(), type);
+  }
   return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(out);
   END_HANDLE_TH_ERRORS
 }
@@ -256,7 +296,6 @@ PyObject* mx4_gemm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   int64_t ld = N;
   if (is_none(a[12])) {
     if (type != DEFL_BF16 && type != DEFL_F32) return PyLong_FromLong(DEFL_ERR_ARG);
-    out = make({b, M, N}, type == DEFL_BF16 ? at::kBFloat16 : at::kFloat, device);
   } else {
     out = tensor(a[12], "out");
     const int64_t want[3] = {b, M, N};
@@ -266,12 +305,17 @@ PyObject* mx4_gemm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     if (M > 1) ld = out.stride(1);
   }
   if (b > 65535) return PyLong_FromLong(DEFL_ERR_RANK);
-  Tensor work;
-  const size_t room = defl_mx4_gemm_work_bytes(c, (int)b, side(M), side(N), side(K), type);
-  if (room) work = make({(int64_t)room}, at::kByte, device);
-  use_stream(c, device);
-  const int rc = defl_mx4_gemm(c, &A, &B, (int)b, side(M), side(N), side(K), bb == 1, fmt, (float)alpha, out.data_ptr(), ld, out.stride(0), type,
-                               room ? work.data_ptr() : nullptr);
+  int rc;
+  {
+    const Unlocked unlocked(c);
+    if (!out.defined()) out = make({b, M, N}, type == DEFL_BF16 ? at::kBFloat16 : at::kFloat, device);
+    Tensor work;
+    const size_t room = defl_mx4_gemm_work_bytes(c, (int)b, side(M), side(N), side(K), type);
+    if (room) work = make({(int64_t)room}, at::kByte, device);
+    use_stream(c, device);
+    rc = defl_mx4_gemm(c, &A, &B, (int)b, side(M), side(N), side(K), bb == 1, fmt, (float)alpha, out.data_ptr(), ld, out.stride(0), type,
+                       room ? work.data_ptr() : nullptr);
+  }
   return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(out);
   END_HANDLE_TH_ERRORS
 }

@@ -48,16 +48,25 @@ def deflation_active(step, total_steps, cutoff=1.0):
     return step < cutoff * total_steps
 
 
+def _look_ahead_has_gradients(weights, grads, nesterov):
+    """The Nesterov look-ahead is formed with the gradient: a group without one is refused before anything has been changed."""
+    if nesterov:
+        for shape in weights:
+            if grads.get(shape) is None:
+                raise ValueError("group %s has no gradient, which nesterov=True needs" % (shape,))
+
+
 def muon_step_groups(ctx, weights, momenta, grads, lr, mu, window, oversample, power_iters, coeff_schedule,
                      step=None, total_steps=None, cutoff=1.0, **kw):
     """One Deflated Muon step over stacked groups: weights/momenta/grads are dicts {(m, n): [b, m, n] tensor} (grads
-    may hold None). `window` is the number k of leading triplets, or a ratio w in (0, 1) meaning k = ceil(w min(m, n));
+    may hold None, unless kw says nesterov=True). `window` is the number k of leading triplets, or a ratio w in (0, 1) meaning k = ceil(w min(m, n));
     `oversample` likewise a count or a ratio delta (Section 3: r = ceil(w m), r' = r + ceil(delta m)). With `step` and
     `total_steps` the deflation cutoff applies: past it the step runs with k = 0, which is the plain Muon step (no
     range finder, no deflation pass, the same filter)."""
     import math
     if step is not None and total_steps is not None and not deflation_active(step, total_steps, cutoff):
         window = 0
+    _look_ahead_has_gradients(weights, grads, kw.get("nesterov"))
     for shape, W in weights.items():
         ms = min(shape)
         k = int(math.ceil(window * ms)) if 0 < window < 1 else int(window)
@@ -72,7 +81,13 @@ def optimizer_step_groups(ctx, weights, momenta, grads, lr, mu, window, oversamp
     gradients together; with max_norm > 0 its factor scales both kinds. rest_step is an int64 CUDA tensor [1], the number of
     AdamW steps taken so far: it is advanced on the device. A norm that is not finite leaves the rest and the counter as they are,
     and the matrices take a step along their momentum without the gradient. `adamw`: further arguments of defl_adamw_step.
-    Nothing waits; returns the tensor (norm, factor)."""
+    Nothing waits; returns the tensor (norm, factor). A missing gradient under nesterov=True and a list of gradients of the wrong
+    length are refused before the counter, the weights or the moments change."""
+    rest_grads = list(rest_grads)
+    _look_ahead_has_gradients(weights, grads, kw.get("nesterov"))
+    sizes = getattr(rest, "sizes", rest_grads)
+    if len(sizes) != len(rest_grads):
+        raise ValueError("%d gradients for %d parameters" % (len(rest_grads), len(sizes)))
     every = [g for g in grads.values() if g is not None] + [g for g in rest_grads if g is not None]
     clip = ctx.defl_grad_norm(every, max_norm, step=rest_step)
     muon_step_groups(ctx, weights, momenta, grads, lr, mu, window, oversample, power_iters, coeff_schedule, grad_scale=clip, **kw)

@@ -38,6 +38,33 @@ def test_one_norm_for_both_kinds():
                          ("adamw", "rest", ["g0", None], 1e-3, "t", "clip", {"eps": 1e-6})]
 
 
+@pytest.mark.parametrize("kw,rest_grads", [(dict(nesterov=True), ["g0", "g1"]), (dict(), ["g0"]), (dict(), ["g0", "g1", "g2"])])
+def test_refused_step_changes_nothing(kw, rest_grads):
+    """A group without a gradient under the Nesterov look-ahead, and gradients that are too few or too many: no call is made, so that neither the
+    counter nor a weight has moved; the Muon groups alone refuse the same."""
+    from paper_2609_21102_b200 import grouping
+
+    class Rest:
+        sizes = [10, 20]
+    rec = Recorder()
+    groups = ({(4, 8): "W", (8, 8): "V"}, {(4, 8): "MW", (8, 8): "MV"}, {(4, 8): "GW", (8, 8): None}, 0.02, 0.95, 1, 1, 1, [[1.0, 0.0, 0.0]])
+    with pytest.raises(ValueError):
+        grouping.optimizer_step_groups(rec, *groups, Rest(), rest_grads, 1e-3, "t", **kw)
+    if kw:
+        with pytest.raises(ValueError):
+            grouping.muon_step_groups(rec, *groups, **kw)
+    assert rec.calls == []
+
+
+def test_gradients_from_a_generator():
+    """The norm and the step read the same gradients, also where they come one after the other."""
+    from paper_2609_21102_b200 import grouping
+    rec = Recorder()
+    grouping.optimizer_step_groups(rec, {}, {}, {}, 0.02, 0.95, 1, 1, 1, [[1.0, 0.0, 0.0]], "rest", (g for g in ("g0", None, "g2")), 1e-3, "t")
+    assert [c[0] for c in rec.calls] == ["norm", "adamw"]
+    assert rec.calls[0][1] == ["g0", "g2"] and rec.calls[1][2] == ["g0", None, "g2"]
+
+
 def _dq(X, fmt):
     return np.stack([mx4.round_trip(x, fmt) for x in X])
 

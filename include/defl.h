@@ -355,7 +355,8 @@ typedef struct defl_adamw_opts {
   int stochastic;
 } defl_adamw_opts;
 
-/* Errors: DEFL_ERR_ARG (null pointers, bad types, a step below 1, hyperparameters out of range), DEFL_ERR_RANK (more than
+/* Errors: DEFL_ERR_ARG (null pointers, pointers that are not multiples of their element's size, bad types, a step below 1,
+ * hyperparameters out of range), DEFL_ERR_RANK (more than
  * 4e12 elements), DEFL_ERR_CUDA. Tensors that do not all start on 16-byte boundaries take single accesses: right, and slower. */
 int defl_adamw_step(defl_ctx* ctx, const defl_adamw_tensor* tensors, int count, const defl_adamw_opts* opts);
 
@@ -366,7 +367,7 @@ int defl_adamw_step(defl_ctx* ctx, const defl_adamw_tensor* tensors, int count, 
  *   tensors  host, `count` of them (n = 0 is skipped);  out  device, [2] fp32;  step  device, NULL or one int64
  *   work     device, defl_grad_norm_work_bytes(count) bytes, 8-byte aligned, of this call alone until it is through: calls that
  *            may run at the same time (two streams, two captured graphs) need one each
- * Errors: DEFL_ERR_ARG, DEFL_ERR_RANK (more than 1.7e13 elements), DEFL_ERR_CUDA. */
+ * Errors: DEFL_ERR_ARG (also for pointers that are not multiples of their element's size), DEFL_ERR_RANK (more than 1.7e13 elements), DEFL_ERR_CUDA. */
 typedef struct defl_norm_tensor {
   const void* x;
   int64_t n;
@@ -391,7 +392,8 @@ int defl_grad_norm(defl_ctx* ctx, const defl_norm_tensor* tensors, int count, fl
  *   scales  [ceil(rows / 128), ceil(blocks / 4), 512] bytes, blocks = W / 32 or W / 16: row r, block c of a tile of 128 rows x 4 blocks at
  *           byte (r % 32) * 16 + (r / 32) * 4 + c, the order in which the tensor cores read them; padding is zeros
  *   scale   [b] fp32 (DEFL_NVFP4; unused with DEFL_MXFP4)
- * Buffers of codes and scales start on 16-byte boundaries; sides are at most DEFL_MX4_MAX_SIDE. */
+ * Buffers of codes and scales start on 16-byte boundaries, `scale` and matrices on multiples of their element's size
+ * (DEFL_ERR_ARG); sides are at most DEFL_MX4_MAX_SIDE. */
 #define DEFL_MXFP4 0
 #define DEFL_NVFP4 1
 #define DEFL_MX4_MAX_SIDE (1 << 23)

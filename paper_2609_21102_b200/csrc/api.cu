@@ -1025,6 +1025,7 @@ int defl_muon_step_batched(defl_ctx* c, void* W, int w_dtype, void* Mom, const v
   if ((dtype != DEFL_BF16 && dtype != DEFL_F32) || (w_dtype != DEFL_BF16 && w_dtype != DEFL_F32)) return DEFL_ERR_ARG;
   if (L < 1 || !coeff_schedule) return DEFL_ERR_ARG;
   if (nesterov && !Grad) return DEFL_ERR_ARG;
+  if (opts && (reinterpret_cast<uintptr_t>(opts->grad_scale) & 3u)) return DEFL_ERR_ARG;
   cudaSetDevice(c->device);
   const size_t count = (size_t)b * m * n;
   int rc = ensure_staging(c, count * dtype_size(dtype));

@@ -587,7 +587,7 @@ struct DeviceScope {
 int partials_of(int b) { return b >= MAX_PARTIALS ? 1 : MAX_PARTIALS / b; }
 
 bool matrix_ok(const defl_mx4* m, int fmt) {
-  return m->codes && m->scales && on(m->codes, 16) && on(m->scales, 16) && (fmt == DEFL_MXFP4 || m->scale);
+  return m->codes && m->scales && on(m->codes, 16) && on(m->scales, 16) && (fmt == DEFL_MXFP4 || (m->scale && on(m->scale, 4)));
 }
 
 }  // namespace

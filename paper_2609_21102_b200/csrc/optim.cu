@@ -432,7 +432,8 @@ __global__ void __launch_bounds__(OPT_THREADS) grad_norm_finish_kernel(const dou
   }
 }
 
-bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool on(const void* p, unsigned a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+bool on16(const void* p) { return on(p, 16); }
 
 template <typename P, typename G, bool EIGHT, bool SR, int CAP>
 cudaError_t adamw_launch(const AdamTable<ADAM_CAP>& tb, int num_sms, cudaStream_t st) {
@@ -509,6 +510,7 @@ int defl_adamw_step(defl_ctx* c, const defl_adamw_tensor* t, int count, const de
   if (!(o->beta1 >= 0.0 && o->beta1 < 1.0) || !(o->beta2 >= 0.0 && o->beta2 < 1.0) || !(o->eps >= 0.0) || !isfinite(o->eps) ||
       !isfinite(o->lr) || !isfinite(o->weight_decay)) return DEFL_ERR_ARG;
   if (!o->step_dev && o->step < 1) return DEFL_ERR_ARG;
+  if (!on(o->step_dev, 8) || !on(o->lr_dev, 4) || !on(o->grad_scale, 4)) return DEFL_ERR_ARG;
   unsigned long long total = 0;
   unsigned int present = 0;                       // the combinations of types that the list holds
   for (int i = 0; i < count; ++i) {
@@ -518,7 +520,9 @@ int defl_adamw_step(defl_ctx* c, const defl_adamw_tensor* t, int count, const de
     if (!x.p || !x.m || !x.v) return DEFL_ERR_ARG;
     if ((x.p_dtype != DEFL_F32 && x.p_dtype != DEFL_BF16) || (x.g_dtype != DEFL_F32 && x.g_dtype != DEFL_BF16)) return DEFL_ERR_ARG;
     if (x.state_bits != 32 && x.state_bits != 8) return DEFL_ERR_ARG;
-    if (x.state_bits == 8 && (!x.m_scale || !x.v_scale)) return DEFL_ERR_ARG;
+    if (x.state_bits == 8 && (!x.m_scale || !x.v_scale || !on(x.m_scale, 4) || !on(x.v_scale, 4))) return DEFL_ERR_ARG;
+    if (!on(x.p, (unsigned)dtype_size(x.p_dtype)) || !on(x.g, (unsigned)dtype_size(x.g_dtype)) || !on(x.copy, 2)) return DEFL_ERR_ARG;
+    if (x.state_bits == 32 && (!on(x.m, 4) || !on(x.v, 4))) return DEFL_ERR_ARG;
     present |= 1u << type_class(x);
     total += (unsigned long long)((x.n + CHUNK - 1) / CHUNK);
   }
@@ -572,12 +576,12 @@ size_t defl_grad_norm_work_bytes(int count) {
 }
 
 int defl_grad_norm(defl_ctx* c, const defl_norm_tensor* t, int count, float max_norm, float* out, int64_t* step, void* work) {
-  if (!c || count < 0 || (count > 0 && !t) || !out || !work || (reinterpret_cast<uintptr_t>(work) & 7u) || isnan(max_norm)) return DEFL_ERR_ARG;
+  if (!c || count < 0 || (count > 0 && !t) || !out || !work || !on(work, 8) || !on(out, 4) || !on(step, 8) || isnan(max_norm)) return DEFL_ERR_ARG;
   unsigned long long total = 0;
   for (int i = 0; i < count; ++i) {
     if (t[i].n < 0 || t[i].n > MAX_ELEMENTS) return DEFL_ERR_ARG;
     if (t[i].n == 0) continue;
-    if (!t[i].x || (t[i].dtype != DEFL_F32 && t[i].dtype != DEFL_BF16)) return DEFL_ERR_ARG;
+    if (!t[i].x || (t[i].dtype != DEFL_F32 && t[i].dtype != DEFL_BF16) || !on(t[i].x, (unsigned)dtype_size(t[i].dtype))) return DEFL_ERR_ARG;
     total += (unsigned long long)((t[i].n + NORM_CHUNK - 1) / NORM_CHUNK);
   }
   if (total > 0x7fffffffull) return DEFL_ERR_RANK;

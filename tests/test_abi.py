@@ -113,3 +113,53 @@ def test_window_ratios_follow_the_algorithms(libpath):
     with pytest.raises(binding.DeflError) as e:
         binding.defl_polar_window(128, 256, -0.1, 0.0)
     assert e.value.code == -1
+
+
+def test_pointers_that_are_not_multiples_of_their_elements_are_refused(libpath):
+    """Decided on the host before anything is launched, so that a block of zeros may stand in for the context."""
+    import numpy as np
+    from paper_2609_21102_b200 import binding
+    L = binding.lib()
+    room = ctypes.create_string_buffer(1 << 20)
+    at = 1 << 12                                             # (an address that nothing reads)
+    fine = dict(p=at, g=at, m=at, v=at, m_scale=at, v_scale=at, copy=at, n=10, p_dtype=binding.F32, g_dtype=binding.F32, state_bits=8)
+
+    class Opts(ctypes.Structure):
+        _fields_ = [(x, ctypes.c_double) for x in ("lr", "beta1", "beta2", "eps", "weight_decay")] + \
+                   [("step", ctypes.c_int64)] + [(x, ctypes.c_void_p) for x in ("step_dev", "lr_dev", "grad_scale")] + \
+                   [("seed", ctypes.c_uint64), ("stochastic", ctypes.c_int)]
+
+    def adamw(opts=None, **kw):
+        t = np.zeros(1, dtype=binding._ADAMW_TENSOR)
+        for key, value in {**fine, **kw}.items():
+            t[key] = value
+        o = Opts(1e-3, 0.9, 0.999, 1e-8, 0.0, 1, **(opts or {}))
+        return L.defl_adamw_step(room, ctypes.c_void_p(t.ctypes.data), 1, ctypes.byref(o))
+    for kw in (dict(p=at + 2), dict(g=at + 2), dict(p=at + 1, p_dtype=binding.BF16), dict(g=at + 1, g_dtype=binding.BF16), dict(copy=at + 1),
+               dict(m_scale=at + 2), dict(v_scale=at + 1), dict(m=at + 2, state_bits=32), dict(v=at + 1, state_bits=32),
+               dict(opts=dict(step_dev=at + 4)), dict(opts=dict(lr_dev=at + 2)), dict(opts=dict(grad_scale=at + 2))):
+        assert adamw(**kw) == -1, kw
+
+    class Norm(ctypes.Structure):
+        _fields_ = [("x", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int)]
+
+    def norm(x=at, dtype=binding.F32, out=at, step=at, work=at):
+        t = Norm(x, 10, dtype)
+        return L.defl_grad_norm(room, ctypes.byref(t), 1, ctypes.c_float(1.0), ctypes.c_void_p(out), ctypes.c_void_p(step), ctypes.c_void_p(work))
+    for kw in (dict(x=at + 2), dict(x=at + 1, dtype=binding.BF16), dict(out=at + 2), dict(step=at + 4), dict(work=at + 4)):
+        assert norm(**kw) == -1, kw
+    # nvfp4's matrix scale, in each of the three calls
+    q, bad = (ctypes.c_void_p * 3)(at, at, at), (ctypes.c_void_p * 3)(at, at, at + 2)
+    i64, p = ctypes.c_int64, ctypes.c_void_p
+    for rows, cols in ((bad, None), (None, bad), (q, bad)):
+        assert L.defl_mx4_quantize(room, p(at), binding.F32, 1, 4, 4, i64(4), i64(16), 1, rows, cols, p(at)) == -1
+    assert L.defl_mx4_dequantize(room, bad, 1, 4, 4, 1, p(at), binding.F32) == -1
+    for a, b in ((bad, q), (q, bad)):
+        assert L.defl_mx4_gemm(room, a, b, 1, 4, 4, 4, 0, 1, ctypes.c_float(1.0), p(at), i64(4), i64(16), binding.F32, None) == -1
+    # the Muon step's factor
+    o = binding.DeflOpts()
+    o.grad_scale = at + 2
+    schedule = (ctypes.c_float * 3)(1.0, 0.0, 0.0)
+    f = ctypes.c_float
+    assert L.defl_muon_step_batched(room, p(at), binding.F32, p(at), p(at), 1, 4, 4, binding.F32, f(0.1), f(0.9), 0, f(0.0), f(1.0), 1, 1, 1,
+                                    schedule, 1, ctypes.byref(o), None) == -1

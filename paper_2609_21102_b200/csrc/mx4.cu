@@ -88,7 +88,8 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t big, float whole, flo
     } else {
       q.r = q.s > 0.f ? __frcp_rn(q.s) : 0.f;
     }
-    if (big >= 0x7f800000u) q.byte = 0x7fu;
+    // NaN; what is finite in such a block, the padding too, becomes zero (a factor made of NaN turned the padding's zeros into sixes)
+    if (big >= 0x7f800000u) { q.byte = 0x7fu; q.r = q.lo = q.s = 0.f; }
   }
   return q;
 }

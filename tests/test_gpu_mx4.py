@@ -453,3 +453,19 @@ def test_wait_that_ran_out_is_not_lost_in_a_later_call(monkeypatch):
     assert held.defl_device_wait_status(clear=False) == binding.ST_DEVICE_WAIT
     assert held.defl_device_wait_status() == binding.ST_DEVICE_WAIT and held.defl_device_wait_status() == 0
     held.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("shape", [(1, 5, 37), (2, 37, 130), (1, 200, 257)])
+def test_padding_of_a_block_that_is_not_finite(ctx, fmt, dtype, bad, shape):
+    """Columns (and for the transpose rows) that do not exist are zeros beside a value that is not finite too, by either way in."""
+    X = _rand(shape, 36, dtype)
+    X[0, 1, -1], X[0, -1, 2] = bad, bad
+    for part in (X.cuda(), torch.nn.functional.pad(X, (0, 7)).cuda()[:, :, :-7]):
+        q, qt = ctx.defl_mx4_quantize(part, fmt, both=True)
+        P = part.double().cpu().numpy()
+        _same(q, P, fmt)
+        _same(qt, P.transpose(0, 2, 1), fmt)

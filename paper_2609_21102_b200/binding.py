@@ -210,23 +210,22 @@ class AdamWGroup:
     """The tensors of defl_adamw_step, checked once: parameters (float32 or bfloat16), first and second moments of the same
     sizes, all float32 or, in 8 bits, float8_e4m3fn with float32 scales [ceil(n / 256)] (the second moment is held as its
     root); optional bfloat16 copies of the parameters. The group keeps the tensors' memory alive; no two of them may overlap.
-    A parameter that has been given other memory since (p.data = ..., .to(...)) is refused: it needs a new group."""
+    A tensor of the group that has been given other memory since (p.data = ..., .to(...)) is refused: it needs a new group, and so
+    do other tensors in its place (the group's lists are tuples)."""
+    params, exp_avg, exp_avg_sq, avg_scale, root_scale, copies = (property(lambda self, i=i: self._lists[i]) for i in range(6))
 
     def __init__(self, params, exp_avg, exp_avg_sq, avg_scale=None, root_scale=None, copies=None):
-        self.params, self.exp_avg, self.exp_avg_sq = list(params), list(exp_avg), list(exp_avg_sq)
-        count = len(self.params)
-        none = [None] * count
-        self.avg_scale = list(avg_scale) if avg_scale is not None else none
-        self.root_scale = list(root_scale) if root_scale is not None else none
-        self.copies = list(copies) if copies is not None else none
-        lists = (self.params, self.exp_avg, self.exp_avg_sq, self.avg_scale, self.root_scale, self.copies)
+        params = tuple(params)
+        count = len(params)
+        self._lists = lists = (params,) + tuple(tuple(x) if x is not None else (None,) * count
+                                                for x in (exp_avg, exp_avg_sq, avg_scale, root_scale, copies))
         if any(len(x) != count for x in lists):
             raise ValueError("the lists of an AdamWGroup must have one entry per parameter")
         # what the table points to stays, whatever becomes of the tensors
-        self._params = tuple(self.params)
+        self._others = []
         self._memory = [[t.detach() for t in x if t is not None] for x in lists]
-        self.device = self.params[0].device if count else None
-        self.sizes = [p.numel() for p in self.params]
+        self.device = params[0].device if count else None
+        self.sizes = [p.numel() for p in params]
         self.table = np.zeros(count, dtype=_ADAMW_TENSOR)
         spans = []
         for i, (p, m, v, ms, vs, c) in enumerate(zip(*lists)):
@@ -250,9 +249,11 @@ class AdamWGroup:
                     raise ValueError("%s %d must have %d elements%s" % (what, i, size, " of " + str(dtype) if dtype else ""))
                 if size:
                     spans.append((t.data_ptr(), t.data_ptr() + size * t.element_size(), "%s %d" % (what, i)))
+            self._others += [t for t, *_ in want[1:]] if n else []
             ptr = lambda t: t.data_ptr() if t is not None else 0  # noqa: E731
             self.table[i] = (ptr(p), 0, ptr(m), ptr(v), ptr(ms) if eight else 0, ptr(vs) if eight else 0, ptr(c), n, _dtype_code(p), F32,
                              8 if eight else 32)
+        self._others = tuple(self._others)
         self.address, self.count = self.table.ctypes.data, count
         spans.sort()
         for a, b in zip(spans, spans[1:]):
@@ -505,8 +506,8 @@ class Context:
         tensor [1]; grad_scale: defl_grad_norm's result, whose factor multiplies the gradients (0: the step is left out)."""
         if group.device is not None and group.device != self.device:
             raise ValueError("the group's tensors are on %s, the context is on %s" % (group.device, self.device))
-        self._check(_native().adamw_step(self._handle, self._index, group.address, group._params, grads, lr, step, betas[0], betas[1], eps,
-                                         weight_decay, grad_scale, stochastic, seed))
+        self._check(_native().adamw_step(self._handle, self._index, group.address, group.params, grads, lr, step, betas[0], betas[1], eps,
+                                         weight_decay, grad_scale, stochastic, seed, group._others))
 
     def _scalar(self, t, dtype, count, what):
         if t.device != self.device or t.dtype != dtype or t.numel() != count or not t.is_contiguous():

@@ -75,10 +75,16 @@ bool gradient(PyObject* o, Py_ssize_t i, int device, const void** x, int64_t* n,
   return true;
 }
 
-// adamw_step(handle, device, table address, params, grads, lr, step, beta1, beta2, eps, weight_decay, grad_scale, stochastic, seed) -> code
+// a tensor of an AdamWGroup is where it was when the group was made (386 parameters: 7 us for their two moments, 12 with scales)
+inline void in_place(const Tensor& t, const void* p, int64_t n, const char* what, Py_ssize_t i) {
+  TORCH_CHECK_VALUE(t.data_ptr() == p && t.numel() == n, what, " ", i, " has other memory than when its AdamWGroup was made");
+}
+
+// adamw_step(handle, device, table address, params, grads, lr, step, beta1, beta2, eps, weight_decay, grad_scale, stochastic, seed[, others]) -> code
+// others: for each parameter that is not empty its moments, their scales in 8 bits, its copy if it has one
 PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
-  TORCH_CHECK(nargs == 14, "adamw_step takes 14 arguments");
+  TORCH_CHECK(nargs == 14 || nargs == 15, "adamw_step takes 14 or 15 arguments");
   defl_ctx* c = handle(a[0]);
   const int device = (int)PyLong_AsLong(a[1]);
   const defl_adamw_tensor* held = reinterpret_cast<const defl_adamw_tensor*>(PyLong_AsVoidPtr(a[2]));
@@ -95,10 +101,32 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   if (PyErr_Occurred()) throw python_error();
   // (a copy for this call, with its gradients: the group's table is shared by all)
   std::vector<defl_adamw_tensor> table(held, held + count);
+  if (nargs == 15) {
+    const Sequence others(a[14]);
+    Py_ssize_t at = 0;
+    auto next = [&](const void* p, int64_t n, const char* what, Py_ssize_t i) {
+      TORCH_CHECK_VALUE(at < others.size(), "tensors of the AdamWGroup are missing");
+      // (the group holds nothing but tensors. 386 to 1544 of them, each behind three pointers: those of a later one are asked for now)
+      if (at + 8 < others.size()) __builtin_prefetch(THPVariable_Unpack(others[at + 8]).unsafeGetTensorImpl());
+      if (at + 4 < others.size()) __builtin_prefetch(THPVariable_Unpack(others[at + 4]).unsafeGetTensorImpl()->unsafe_storage().unsafeGetStorageImpl());
+      in_place(THPVariable_Unpack(others[at++]), p, n, what, i);
+    };
+    for (Py_ssize_t i = 0; i < count; ++i) {
+      const defl_adamw_tensor& t = table[i];
+      const int64_t blocks = (t.n + 255) / 256;
+      if (t.n == 0) continue;
+      next(t.m, t.n, "first moment", i);
+      next(t.v, t.n, "second moment", i);
+      if (t.state_bits == 8) {
+        next(t.m_scale, blocks, "first moment's scales", i);
+        next(t.v_scale, blocks, "second moment's scales", i);
+      }
+      if (t.copy) next(t.copy, t.n, "copy", i);
+    }
+  }
   for (Py_ssize_t i = 0; i < count; ++i) {
     int64_t n = 0;
-    const Tensor& p = tensor(params[i], "a parameter");
-    TORCH_CHECK_VALUE(p.data_ptr() == table[i].p && p.numel() == table[i].n, "parameter ", i, " has other memory than when its AdamWGroup was made");
+    in_place(tensor(params[i], "a parameter"), table[i].p, table[i].n, "parameter", i);
     table[i].g = nullptr;
     if (!gradient(grads[i], i, device, &table[i].g, &n, &table[i].g_dtype)) continue;
     TORCH_CHECK_VALUE(n == table[i].n, "gradient ", i, " has ", n, " elements, its parameter ", table[i].n);

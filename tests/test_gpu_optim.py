@@ -319,6 +319,32 @@ def test_a_parameter_that_has_moved(ctx):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("which", ["first moment", "second moment", "first moment's scales", "second moment's scales", "copy"])
+def test_a_moment_that_has_moved(ctx, which):
+    """What belongs to a parameter and was given other memory since its group was made is refused, by its name, and nothing is updated."""
+    from paper_2609_21102_b200 import binding
+    e8 = torch.float8_e4m3fn
+    f = lambda n, dtype=F32: torch.zeros(n, dtype=dtype, device="cuda")  # noqa: E731
+    parts = {"parameter": f(700), "first moment": f(700, e8), "second moment": f(700, e8), "first moment's scales": f(3),
+             "second moment's scales": f(3), "copy": f(700, BF16)}
+    group = binding.AdamWGroup([f(9)] + [parts["parameter"]], [f(9)] + [parts["first moment"]], [f(9)] + [parts["second moment"]],
+                               [None, parts["first moment's scales"]], [None, parts["second moment's scales"]], copies=[None, parts["copy"]])
+    grads = [torch.ones(9, device="cuda"), torch.ones(700, device="cuda")]
+    ctx.defl_adamw_step(group, grads, LR, 1)
+    moved = parts[which]
+    moved.data = moved.data.clone()
+    held = [t.clone() for t in list(group.params) + list(parts.values())]
+    with pytest.raises(ValueError, match="%s 1 has other memory" % which):
+        ctx.defl_adamw_step(group, grads, LR, 2)
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(held, list(group.params) + list(parts.values())))
+    for name, place in (("params", 0), ("exp_avg", 1)):      # another tensor in its place would not be seen either
+        with pytest.raises(TypeError):
+            getattr(group, name)[place] = moved
+        with pytest.raises(AttributeError):
+            setattr(group, name, [moved])
+
+
+@pytest.mark.gpu
 def test_smallest_eps(ctx):
     """An eps below fp32's normal numbers is zero; where both moments are, the quotient is then NaN, as 0 / 0 is."""
     from paper_2609_21102_b200 import binding

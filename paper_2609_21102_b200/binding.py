@@ -260,6 +260,9 @@ class AdamWGroup:
             if b[0] < a[1]:
                 raise ValueError("%s and %s overlap" % (a[2], b[2]))
 
+    def __reduce_ex__(self, protocol):
+        raise TypeError("an AdamWGroup holds addresses and is not copied or pickled: make one of the copied tensors")
+
 
 class Context:
     """defl_ctx bound to one CUDA device; work is enqueued on torch's current stream at call time."""

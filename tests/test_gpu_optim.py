@@ -431,3 +431,14 @@ def test_refusals_without_a_device():
         binding._native().grad_norm(0, 0, [3], 1.0, None, None)
     with pytest.raises(ValueError):
         binding._native().adamw_step(0, 0, 0, [torch.zeros(3)], [], 1e-3, 1, 0.9, 0.999, 1e-8, 0.0, None, False, 0)
+
+
+def test_a_group_is_not_copied():
+    """A copy would hold the addresses of the original's table and tensors, and outlive them."""
+    import copy
+    import pickle
+    from paper_2609_21102_b200 import binding
+    group = binding.AdamWGroup([], [], [])
+    for f in (copy.copy, copy.deepcopy, pickle.dumps):
+        with pytest.raises(TypeError):
+            f(group)

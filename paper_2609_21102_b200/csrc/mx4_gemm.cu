@@ -575,8 +575,11 @@ __global__ void __launch_bounds__(ROW_THREADS) mx4_row_kernel(const RowParams p)
               pos = __dp4a((int)lookup(x >> 16), ah, pos);
               neg = __dp4a((int)lookup((x >> 16) ^ 0x8888u), ah, neg);
             }
-            // (the sum meets one scale after the other: their product alone may leave fp32's range)
-            sum[t] += (float)(pos - neg) * s_sc[t][(i - first) * NB + h] * scale_value<FMT>(h ? cur_sb[k] >> 8 : cur_sb[k] & 0xffu);
+            const float sa = s_sc[t][(i - first) * NB + h], sb = scale_value<FMT>(h ? cur_sb[k] >> 8 : cur_sb[k] & 0xffu);
+            // The sum meets one scale after the other: their product alone may leave fp32's range. mxfp4, the smaller one first: that product is
+            // exact (an integer times at least 2^-129), and the sum times the larger one alone may be past fp32 where the result is not.
+            const bool up = FMT == MXFP4 && sb < sa;               // (false beside a NaN, which stays in either place)
+            sum[t] += (float)(pos - neg) * (up ? sb : sa) * (up ? sa : sb);
           }
         }
       }

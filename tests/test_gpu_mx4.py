@@ -469,3 +469,22 @@ def test_padding_of_a_block_that_is_not_finite(ctx, fmt, dtype, bad, shape):
         P = part.double().cpu().numpy()
         _same(q, P, fmt)
         _same(qt, P.transpose(0, 2, 1), fmt)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [1, 2, 3, 8, 9, 200])
+@pytest.mark.parametrize("up", [120, 100, -120])
+def test_mxfp4_rows_far_apart_in_size(ctx, rows, up):
+    """A near 2^up and B near 2^-up: a block's sum times one of its two scales may leave fp32 (32 products of at least 9 times 2^120), times
+    both it is an ordinary number. Grid values with a six in every block: the sums are exact and so is the result."""
+    rng = np.random.default_rng(37)
+
+    def make(n):
+        x = rng.choice([3.0, 4.0, 6.0], (1, n, 352))
+        x[:, :, ::32] = 6.0
+        return torch.tensor(x, dtype=F32).cuda()
+    a, w = make(rows), make(90)
+    A, B = ctx.defl_mx4_quantize(a * 2.0 ** up, "mxfp4"), ctx.defl_mx4_quantize(w * 2.0 ** -up, "mxfp4")
+    want = a.double() @ w.double().transpose(1, 2)
+    assert torch.equal(ctx.defl_mx4_gemm(A, B, out_dtype=F32).double(), want)
+    assert torch.equal(ctx.defl_mx4_gemm(B, A, out_dtype=F32).double(), want.transpose(1, 2))

@@ -55,7 +55,7 @@ struct TcParams4 {
   void* D; long long ldd, batch_d;
   float alpha; const float* scale_a; const float* scale_b;
   int* status; unsigned long long wait_ns;
-  int hold;                                        // test hook: the codes of every CTA's first stage are neither announced nor copied
+  int hold;                                        // test hook: no codes are announced or copied
 };
 
 // alpha and the matrices' scales in one factor, and `pre`, 1 except where that factor leaves the middle of fp32's range: two matrices of values
@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
     const CUtensorMap* tm = lane == 0 ? &p.tmA : &p.tmB;
     const uint32_t off = lane == 0 ? 0u : p.a_bytes;
     uint32_t stage = 0, phase = 0;
-    bool live = true;
+    bool live = !p.hold;
     pdl_wait();
     for (int tile = tile0; tile < p.total_tiles && live; tile += tile_step) {
       const Tile4 t = tile_of<PAIR>(p, tile);
@@ -210,9 +210,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
         if (lane == 0) ok = mbar_wait(empty0 + 8u * stage, phase ^ 1u, &abort_flag, p.status, p.wait_ns) ? 1 : 0;
         ok = __shfl_sync(0xffffffffu, ok, 0);
         if (!ok) { live = false; break; }
-        const bool held = p.hold && tile == tile0 && kb == t.k0;
-        if (lane == 0 && rank == 0 && !held) mbar_expect_tx(full0 + 8u * stage, tx);
-        if (lane < 2 && !held) {
+        if (lane == 0 && rank == 0) mbar_expect_tx(full0 + 8u * stage, tx);
+        if (lane < 2) {
           const uint32_t dst = smem_base + stage * p.stage_bytes + off;
           if (PAIR) tma_load_3d_pair(dst, tm, full0_sig + 8u * stage, kb * KB_BYTES, c1, c2);
           else tma_load_3d(dst, tm, full0 + 8u * stage, kb * KB_BYTES, c1, c2);
@@ -353,8 +352,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) mx4_tc_kernel(const __grid_cons
       float alpha = p.alpha, pre = 1.f;
       if (FMT == NVFP4 && p.splits == 1) alpha = output_factor(alpha, p.scale_a[t.bz], p.scale_b[p.b_shared ? 0 : t.bz], pre);
       const int out_z = t.ks * p.batch + t.bz;
-      // (the warp goes on or gives up as one: what follows needs all its lanes)
-      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&acc_full_bar[acc]), use, &abort_flag, p.status, p.wait_ns))) break;
+      if (!mbar_wait(smem_u32(&acc_full_bar[acc]), use, &abort_flag, p.status, p.wait_ns)) break;
       tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (acc ? acc1 : 0u);
       const int row0 = t.tm * TILE_M + (int)rank * 128 + q * 32, n0 = t.tn * p.BN;

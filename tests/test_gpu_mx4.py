@@ -412,8 +412,8 @@ def test_refusals_and_sizes_without_a_device():
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("shape", [(1, 64, 64, 64), (1, 300, 256, 512), (2, 700, 600, 4000), (1, 9, 7, 2300)])
 def test_bounded_wait_runs_out_and_is_reported(monkeypatch, ctx, fmt, shape):
-    """A wait that nothing satisfies ends in a status bit and a normal return: the codes of every CTA's first stage are neither announced
-    nor copied, with the limit at 2 ms (one CTA a tile, pairs, several tiles a pair, parts along K). What was asked for has landed long
+    """A wait that nothing satisfies ends in a status bit and a normal return: no codes are announced or copied, with the
+    limit at 2 ms (one CTA a tile, pairs, several tiles a pair, parts along K). What was asked for has landed long
     before the waits give up; the word stays until it is cleared and the context stays usable."""
     from paper_2609_21102_b200 import binding
     b, M, N, K = shape

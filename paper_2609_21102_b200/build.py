@@ -1,7 +1,9 @@
-"""Builds the CUDA library in-tree: paper_2609_21102_b200/libdeflpolar.so (sm_100a only)."""
+"""Builds the CUDA library in-tree, paper_2609_21102_b200/libdeflpolar.so (sm_100a only), and the Python module over it."""
 import os
+import shutil
 import subprocess
 import sys
+import warnings
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -53,20 +55,35 @@ def build(force=False, verbose=False):
 
 
 def build_native(force=False):
-    """The Python module that calls the library without ctypes (csrc/native.cpp), against the installed torch's headers."""
-    src = os.path.join(CSRC, "native.cpp")
-    if not (force or _stale(NATIVE, [src, os.path.join(os.path.dirname(HERE), "include", "defl.h")])):
-        return NATIVE
+    """The Python module that calls the library without ctypes (csrc/native.cpp), against the installed torch's headers. Its ABI is that of
+    the torch and the Python it was built with, whose versions stand beside it. Where a compiler or headers are missing the library
+    serves without it: a warning here, an ImportError from the calls that need it."""
     import sysconfig
     import torch
-    root = os.path.dirname(torch.__file__)
+    src, built_with = os.path.join(CSRC, "native.cpp"), NATIVE + ".versions"
+    versions = "torch %s, python %s\n" % (torch.__version__, sys.version)
+    same = os.path.exists(built_with) and open(built_with).read() == versions
+    if same and not (force or _stale(NATIVE, [src, os.path.join(os.path.dirname(HERE), "include", "defl.h")])):
+        return NATIVE
+    for old in (NATIVE, built_with):
+        if os.path.exists(old):
+            os.remove(old)
+    root, python = os.path.dirname(torch.__file__), sysconfig.get_paths()["include"]
+    missing = [x for x in (os.path.join(python, "Python.h"), os.path.join(root, "include", "torch", "csrc", "autograd", "python_variable.h"))
+               if not os.path.exists(x)] + ([] if shutil.which("g++") else ["g++"])
+    if missing:
+        warnings.warn("%s not built, AdamW, the gradient norm and the 4-bit operators cannot be called from Python: no %s"
+                      % (os.path.basename(NATIVE), ", ".join(missing)))
+        return None
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-w", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
            "-I" + os.path.join(root, "include"), "-I" + os.path.join(root, "include", "torch", "csrc", "api", "include"),
-           "-I" + sysconfig.get_paths()["include"], "-I/usr/local/cuda/include", src, "-o", NATIVE,
+           "-I" + python, "-I/usr/local/cuda/include", src, "-o", NATIVE,
            # torch's libraries are in the process already; the library is found beside the module
            "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda",
            "-L" + HERE, "-l:libdeflpolar.so", "-Wl,-rpath,$ORIGIN"]
     subprocess.run(cmd, check=True)
+    with open(built_with, "w") as f:
+        f.write(versions)
     return NATIVE
 
 

@@ -163,3 +163,30 @@ def test_pointers_that_are_not_multiples_of_their_elements_are_refused(libpath):
     f = ctypes.c_float
     assert L.defl_muon_step_batched(room, p(at), binding.F32, p(at), p(at), 1, 4, 4, binding.F32, f(0.1), f(0.9), 0, f(0.0), f(1.0), 1, 1, 1,
                                     schedule, 1, ctypes.byref(o), None) == -1
+
+
+def test_native_module_follows_its_torch_and_can_be_missing(libpath, monkeypatch, tmp_path):
+    """Built again when the torch or the Python it was built with is another; where no compiler or header is found, the library's build stands
+    and an old module does not. (The commands are recorded, not run.)"""
+    import shutil
+    import torch
+    from paper_2609_21102_b200 import build
+    assert build.build_native() == build.NATIVE and os.path.exists(build.NATIVE)
+    target, ran = str(tmp_path / "_native.so"), []
+
+    def run(cmd, check):
+        ran.append(cmd)
+        open(cmd[cmd.index("-o") + 1], "w").close()
+    monkeypatch.setattr(build, "NATIVE", target)
+    monkeypatch.setattr(build.subprocess, "run", run)
+    assert build.build_native() == target and len(ran) == 1
+    assert build.build_native() == target and len(ran) == 1
+    monkeypatch.setattr(torch, "__version__", "0.0.1")
+    assert build.build_native() == target and len(ran) == 2
+    assert build.build_native() == target and len(ran) == 2
+    monkeypatch.setattr(shutil, "which", lambda name: None)
+    assert build.build_native() == target                    # nothing to do
+    monkeypatch.setattr(torch, "__version__", "0.0.2")
+    with pytest.warns(UserWarning, match=r"no g\+\+"):
+        assert build.build_native() is None
+    assert len(ran) == 2 and not os.path.exists(target)

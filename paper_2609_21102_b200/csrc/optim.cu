@@ -453,7 +453,8 @@ cudaError_t adamw_launch(const AdamTable<ADAM_CAP>& tb, int num_sms, cudaStream_
 template <typename P, typename G, int CAP>
 cudaError_t adamw_pick(const AdamTable<ADAM_CAP>& tb, bool eight, bool sr, int sms, cudaStream_t st) {
   if (eight) return sr ? adamw_launch<P, G, true, true, CAP>(tb, sms, st) : adamw_launch<P, G, true, false, CAP>(tb, sms, st);
-  if (sr && sizeof(P) == 2) return adamw_launch<P, G, false, true, CAP>(tb, sms, st);
+  if constexpr (sizeof(P) == 2)                   // (with fp32 weights and 32-bit moments nothing is left to round)
+    if (sr) return adamw_launch<P, G, false, true, CAP>(tb, sms, st);
   return adamw_launch<P, G, false, false, CAP>(tb, sms, st);
 }
 template <int CAP>

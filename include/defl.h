@@ -397,6 +397,7 @@ int defl_grad_norm(defl_ctx* ctx, const defl_norm_tensor* tensors, int count, fl
 #define DEFL_MXFP4 0
 #define DEFL_NVFP4 1
 #define DEFL_MX4_MAX_SIDE (1 << 23)
+#define DEFL_MX4_SCAN_MOST 32768    /* DEFL_NVFP4: matrices of up to so many elements need no `work` to be quantised */
 typedef struct defl_mx4 {
   void* codes;
   void* scales;
@@ -412,7 +413,8 @@ size_t defl_mx4_work_bytes(int b);
  *   by_cols  blocks along the rows of X: its transpose [cols, rows], for a product that contracts rows; NULL: not wanted
  * A linear layer y = x w^T trains with x, w and dy in both directions: y = x w^T from by_rows of both, dx = dy w from dy's by_rows
  * and w's by_cols, dw = dy^T x from both by_cols. (The gradient of the rounding itself is taken as one.)
- *   work  device, defl_mx4_work_bytes(b) bytes, of this call alone until it is through; unused with DEFL_MXFP4 (may be NULL)
+ *   work  device, defl_mx4_work_bytes(b) bytes, of this call alone until it is through; unused (may be NULL) with DEFL_MXFP4 and for
+ *         matrices of up to DEFL_MX4_SCAN_MOST elements
  * Errors: DEFL_ERR_ARG, DEFL_ERR_RANK (a side above DEFL_MX4_MAX_SIDE, b above 65535), DEFL_ERR_CUDA. */
 int defl_mx4_quantize(defl_ctx* ctx, const void* X, int dtype, int b, int rows, int cols, int64_t ld, int64_t batch_stride, int fmt,
                       const defl_mx4* by_rows, const defl_mx4* by_cols, void* work);

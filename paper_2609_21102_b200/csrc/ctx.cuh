@@ -40,6 +40,17 @@ struct defl_ctx {
 };
 
 namespace defl {
+// the calling thread's current device is put back when a call returns
+struct DeviceScope {
+  int prev = 0;
+  explicit DeviceScope(int dev) {
+    cudaGetDevice(&prev);
+    if (prev != dev) cudaSetDevice(dev); else prev = -1;
+  }
+  ~DeviceScope() { if (prev >= 0) cudaSetDevice(prev); }
+};
+inline bool on(const void* p, unsigned a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }      // starts on a multiple of a
+
 constexpr int WAIT_MX4 = 2, WAIT_WORDS = 3;
 size_t align_up(size_t x, size_t a);
 bool ctx_fail(defl_ctx* c, cudaError_t e, const char* where);

@@ -13,7 +13,6 @@ namespace {
 constexpr int TILE = 128;                  // a CTA takes 128 x 128 values: a whole tile of scales in either direction
 constexpr int Q_THREADS = 256;
 constexpr int MAX_PARTIALS = 592;          // partial maxima a call (four CTAs an SM), at least one a matrix
-constexpr int SCAN_MOST = 32768;           // matrices up to this size: every CTA finds the largest magnitude by itself
 
 struct QuantParams {
   const void* X;
@@ -513,8 +512,7 @@ __global__ void __launch_bounds__(Q_THREADS) mx4_dequantize_kernel(Mx4View a, in
   O* const dst = out + id * cols;
   auto scale_of = [&](int blk) {
     const uint32_t byte = sc[(long long)(blk >> 2) * 512 + (blk & 3)];
-    if (FMT == MXFP4) return byte == 255u ? __uint_as_float(0x7fffffffu) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
-    return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)byte, __NV_E4M3))) * whole;
+    return FMT == MXFP4 ? scale_value<FMT>(byte) : scale_value<FMT>(byte) * whole;
   };
   if (!vec) {
     // rows that do not start on 16-byte boundaries: a value a lane, side by side
@@ -574,17 +572,6 @@ cudaError_t quantize_limit() {
   return e != cudaSuccess ? e : cudaFuncSetAttribute(mx4_quantize_kernel<T, FMT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, quantize_smem<T, FMT>());
 }
 
-bool on(const void* p, unsigned a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-struct DeviceScope {
-  int prev = 0;
-  explicit DeviceScope(int dev) {
-    cudaGetDevice(&prev);
-    if (prev != dev) cudaSetDevice(dev); else prev = -1;
-  }
-  ~DeviceScope() { if (prev >= 0) cudaSetDevice(prev); }
-};
-
 int partials_of(int b) { return b >= MAX_PARTIALS ? 1 : MAX_PARTIALS / b; }
 
 bool matrix_ok(const defl_mx4* m, int fmt) {
@@ -624,7 +611,8 @@ int defl_mx4_quantize(defl_ctx* c, const void* X, int dtype, int b, int rows, in
   const unsigned es = (unsigned)dtype_size(dtype);
   if (!on(X, es)) return DEFL_ERR_ARG;
   if (rows > DEFL_MX4_MAX_SIDE || cols > DEFL_MX4_MAX_SIDE || b > 65535) return DEFL_ERR_RANK;
-  const bool scan = (long long)rows * cols <= SCAN_MOST;
+  const bool scan = (long long)rows * cols <= DEFL_MX4_SCAN_MOST;    // every CTA finds the largest magnitude by itself
+  static_assert(DEFL_MX4_SCAN_MOST <= 0x7fffffff, "the kernel counts these values in 32 bits");
   if (fmt == DEFL_NVFP4 && !scan && (!work || !on(work, 4))) return DEFL_ERR_ARG;
   DeviceScope scope(c->device);
   c->err[0] = 0;

@@ -470,11 +470,6 @@ __device__ __forceinline__ uint32_t lookup(uint32_t sel) {
   asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(0x03020100u), "r"(0x0C080604u), "r"(sel));
   return r;
 }
-template <int FMT>
-__device__ __forceinline__ float scale_value(uint32_t byte) {
-  if (FMT == MXFP4) return byte == 255u ? __uint_as_float(0x7fffffffu) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
-  return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)byte, __NV_E4M3)));
-}
 
 struct RowParams {
   Mx4View A, B;

@@ -250,7 +250,7 @@ PyObject* mx4_quantize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     const defl_mx4 *r = by_rows ? &by_rows->ref : nullptr, *t = by_cols ? &by_cols->ref : nullptr;
     if (turned) std::swap(r, t);
     Tensor work;
-    if (fmt == DEFL_NVFP4 && rows * cols > 32768) work = make({(int64_t)defl_mx4_work_bytes((int)b)}, at::kByte, device);
+    if (fmt == DEFL_NVFP4 && rows * cols > DEFL_MX4_SCAN_MOST) work = make({(int64_t)defl_mx4_work_bytes((int)b)}, at::kByte, device);
     use_stream(c, device);
     rc = defl_mx4_quantize(c, X.data_ptr(), code_of(X.scalar_type()), (int)b, (int)rows, (int)cols, sr, X.stride(0), fmt, r, t,
                            work.defined() ? work.data_ptr() : nullptr);

@@ -432,7 +432,6 @@ __global__ void __launch_bounds__(OPT_THREADS) grad_norm_finish_kernel(const dou
   }
 }
 
-bool on(const void* p, unsigned a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 bool on16(const void* p) { return on(p, 16); }
 
 template <typename P, typename G, bool EIGHT, bool SR, int CAP>
@@ -487,16 +486,6 @@ constexpr long long MAX_ELEMENTS = 1ll << 40;
 int type_class(const defl_adamw_tensor& x) {
   return (x.p_dtype == DEFL_BF16 ? 4 : 0) + (x.g_dtype == DEFL_BF16 ? 2 : 0) + (x.state_bits == 8 ? 1 : 0);
 }
-
-// the calling thread's current device is put back when a call returns
-struct DeviceScope {
-  int prev = 0;
-  explicit DeviceScope(int dev) {
-    cudaGetDevice(&prev);
-    if (prev != dev) cudaSetDevice(dev); else prev = -1;
-  }
-  ~DeviceScope() { if (prev >= 0) cudaSetDevice(prev); }
-};
 
 }  // namespace
 

@@ -113,9 +113,8 @@ typedef struct defl_opts {
                             X <- a_0 X + a_1 (X X^T) X + ... + a_d (X X^T)^d X with d = poly_terms - 1 (4 = the
                             degree-seven member); the schedule is then [L][poly_terms]. The polynomial in the Gram
                             matrix is formed by Horner steps, one more short-side product per degree beyond the quintic. */
-  const float* grad_scale; /* Muon step: device, NULL or a factor of Grad (defl_grad_norm's out + 1): Mom <- mu Mom + c Grad, the
-                            product c Grad rounded to fp32. c = 0 takes Grad as zeros, whatever it holds. */
-} defl_opts;
+} defl_opts;             /* (no size field: it stays as it is, since the calls would read past the end of one of an earlier header;
+                            what comes later is a call or an argument of its own) */
 
 typedef struct defl_info {
   float* s;      /* device, [b, l]: all l estimated singular values, descending (PSD: [K] Ritz values by
@@ -209,6 +208,14 @@ int defl_muon_step_batched(defl_ctx* ctx, void* W, int w_dtype, void* Mom, const
                            int dtype, float lr, float mu, int nesterov, float weight_decay, float scale,
                            int k, int oversample, int power_iters, const float* coeff_schedule, int L,
                            const defl_opts* opts, const defl_info* info);
+
+/* The same step with a factor of Grad: Mom <- mu * Mom + c * Grad (and Nesterov's D with c * Grad), c = *grad_scale, a
+ * device float (defl_grad_norm's out + 1) or NULL for 1; the product c * Grad is rounded to fp32. c = 0 takes Grad as zeros, whatever it
+ * holds. Errors as defl_muon_step_batched; DEFL_ERR_ARG also for a grad_scale that is not a multiple of 4. */
+int defl_muon_step_scaled(defl_ctx* ctx, void* W, int w_dtype, void* Mom, const void* Grad, int b, int m, int n,
+                          int dtype, float lr, float mu, int nesterov, float weight_decay, float scale,
+                          int k, int oversample, int power_iters, const float* coeff_schedule, int L,
+                          const defl_opts* opts, const defl_info* info, const float* grad_scale);
 
 /* Batched randomized SVD alone (Algorithm 3) in the caller's orientation:
  *   G ~ P diag(s) W^T with P [b,m,l], s [b,l] descending, W [b,n,l], all fp32; l = min(min(m,n), k+oversample).

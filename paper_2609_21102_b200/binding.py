@@ -29,7 +29,7 @@ CLASSICAL_QUINTIC = (1.875, -1.25, 0.375)
 
 EXPORTS = [
     "defl_create", "defl_destroy", "defl_set_stream", "defl_polar_workspace_bytes", "defl_psd_workspace_bytes",
-    "defl_polar_window", "defl_psd_window", "defl_polar_batched", "defl_polar_batched_host", "defl_muon_step_batched", "defl_brsvd_batched", "defl_psd_project", "defl_inv_root", "defl_admm_diag_sdp", "defl_fill_gaussian", "defl_debug_gemm",
+    "defl_polar_window", "defl_psd_window", "defl_polar_batched", "defl_polar_batched_host", "defl_muon_step_batched", "defl_muon_step_scaled", "defl_brsvd_batched", "defl_psd_project", "defl_inv_root", "defl_admm_diag_sdp", "defl_fill_gaussian", "defl_debug_gemm",
     "defl_frobenius_norms_noalloc", "defl_set_profiling", "defl_get_stage_ms", "defl_get_stage_ms_sum", "defl_launch_count", "defl_device_wait_status",
     "defl_status_string", "defl_last_error", "defl_adamw_step", "defl_grad_norm", "defl_grad_norm_work_bytes",
     "defl_mx4_codes_bytes", "defl_mx4_scales_bytes", "defl_mx4_work_bytes", "defl_mx4_quantize", "defl_mx4_dequantize", "defl_mx4_gemm", "defl_mx4_gemm_work_bytes",
@@ -41,7 +41,7 @@ class DeflOpts(ctypes.Structure):
                 ("gamma", ctypes.c_float), ("norm_mode", ctypes.c_int), ("lanczos_start", ctypes.c_void_p),
                 ("warmup", ctypes.c_int), ("engine", ctypes.c_int), ("exploit_symmetry", ctypes.c_int),
                 ("tau", ctypes.c_float), ("half_filter", ctypes.c_int), ("bf16_iterates", ctypes.c_int),
-                ("poly_terms", ctypes.c_int), ("grad_scale", ctypes.c_void_p)]
+                ("poly_terms", ctypes.c_int)]
 
 
 # a defl_adamw_tensor, laid out as the C compiler does
@@ -80,6 +80,7 @@ def lib():
         L.defl_muon_step_batched.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p] + [
             ctypes.c_int] * 4 + [ctypes.c_float, ctypes.c_float, ctypes.c_int, ctypes.c_float, ctypes.c_float] + [
             ctypes.c_int] * 3 + [ctypes.POINTER(ctypes.c_float), ctypes.c_int, ctypes.POINTER(DeflOpts), ctypes.POINTER(DeflInfo)]
+        L.defl_muon_step_scaled.argtypes = L.defl_muon_step_batched.argtypes + [ctypes.c_void_p]
         L.defl_brsvd_batched.argtypes = [ctypes.c_void_p, ctypes.c_void_p] + [ctypes.c_int] * 7 + [
             ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.POINTER(DeflOpts), ctypes.c_void_p]
         L.defl_psd_project.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int,
@@ -297,9 +298,8 @@ class Context:
 
     def _opts(self, sketch=None, seed=0, restore_mode=RESTORE_PADDED, gamma=0.0, norm_mode=NORM_LANCZOS,
               lanczos_start=None, warmup=False, engine=ENGINE_AUTO, exploit_symmetry=False, tau=0.0, half_filter=False, bf16_iterates=False,
-              poly_terms=0, grad_scale=None):
+              poly_terms=0):
         o = DeflOpts()
-        o.grad_scale = self._scalar(grad_scale, torch.float32, 2, "grad_scale").data_ptr() + 4 if grad_scale is not None else None
         o.sketch = sketch.data_ptr() if sketch is not None else None
         o.seed = seed
         o.restore_mode = restore_mode
@@ -371,11 +371,12 @@ class Context:
             if sketch.dtype != torch.float32:
                 raise TypeError("sketch must be float32")
         opts = self._opts(sketch=sketch, seed=seed, restore_mode=restore_mode, gamma=gamma, engine=engine,
-                          exploit_symmetry=exploit_symmetry, tau=tau, grad_scale=grad_scale)
+                          exploit_symmetry=exploit_symmetry, tau=tau)
+        factor = self._scalar(grad_scale, torch.float32, 2, "grad_scale").data_ptr() + 4 if grad_scale is not None else None
         self._sync_stream()
-        rc = lib().defl_muon_step_batched(self._h, _ptr(W), _dtype_code(W), _ptr(Mom), _ptr(Grad) if Grad is not None else None,
-                                          b, m, n, _dtype_code(Mom), lr, mu, int(bool(nesterov)), weight_decay, scale,
-                                          k, oversample, power_iters, sched, L, ctypes.byref(opts), None)
+        rc = lib().defl_muon_step_scaled(self._h, _ptr(W), _dtype_code(W), _ptr(Mom), _ptr(Grad) if Grad is not None else None,
+                                         b, m, n, _dtype_code(Mom), lr, mu, int(bool(nesterov)), weight_decay, scale,
+                                         k, oversample, power_iters, sched, L, ctypes.byref(opts), None, factor)
         self._check(rc)
         return W
 

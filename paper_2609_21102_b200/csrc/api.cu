@@ -1021,11 +1021,19 @@ int defl_muon_step_batched(defl_ctx* c, void* W, int w_dtype, void* Mom, const v
                            int dtype, float lr, float mu, int nesterov, float weight_decay, float scale, int k,
                            int oversample, int power_iters, const float* coeff_schedule, int L,
                            const defl_opts* opts, const defl_info* info) {
+  return defl_muon_step_scaled(c, W, w_dtype, Mom, Grad, b, m, n, dtype, lr, mu, nesterov, weight_decay, scale, k, oversample, power_iters,
+                               coeff_schedule, L, opts, info, nullptr);
+}
+
+int defl_muon_step_scaled(defl_ctx* c, void* W, int w_dtype, void* Mom, const void* Grad, int b, int m, int n,
+                          int dtype, float lr, float mu, int nesterov, float weight_decay, float scale, int k,
+                          int oversample, int power_iters, const float* coeff_schedule, int L,
+                          const defl_opts* opts, const defl_info* info, const float* grad_scale) {
   if (!c || !W || !Mom || b <= 0 || m <= 0 || n <= 0) return DEFL_ERR_ARG;
   if ((dtype != DEFL_BF16 && dtype != DEFL_F32) || (w_dtype != DEFL_BF16 && w_dtype != DEFL_F32)) return DEFL_ERR_ARG;
   if (L < 1 || !coeff_schedule) return DEFL_ERR_ARG;
   if (nesterov && !Grad) return DEFL_ERR_ARG;
-  if (opts && (reinterpret_cast<uintptr_t>(opts->grad_scale) & 3u)) return DEFL_ERR_ARG;
+  if (!on(grad_scale, 4)) return DEFL_ERR_ARG;
   cudaSetDevice(c->device);
   const size_t count = (size_t)b * m * n;
   int rc = ensure_staging(c, count * dtype_size(dtype));
@@ -1034,8 +1042,7 @@ int defl_muon_step_batched(defl_ctx* c, void* W, int w_dtype, void* Mom, const v
   const void* D = Mom;
   if (Grad) {
     void* look = nesterov ? c->stage_in : nullptr;
-    if (ctx_fail(c, momentum_launch(Mom, Grad, look, dtype, (long long)count, mu, c->stream, &c->launches,
-                                     opts ? opts->grad_scale : nullptr), "momentum"))
+    if (ctx_fail(c, momentum_launch(Mom, Grad, look, dtype, (long long)count, mu, c->stream, &c->launches, grad_scale), "momentum"))
       return DEFL_ERR_CUDA;
     if (nesterov) D = look;
   }

@@ -157,12 +157,10 @@ def test_pointers_that_are_not_multiples_of_their_elements_are_refused(libpath):
     for a, b in ((bad, q), (q, bad)):
         assert L.defl_mx4_gemm(room, a, b, 1, 4, 4, 4, 0, 1, ctypes.c_float(1.0), p(at), i64(4), i64(16), binding.F32, None) == -1
     # the Muon step's factor
-    o = binding.DeflOpts()
-    o.grad_scale = at + 2
     schedule = (ctypes.c_float * 3)(1.0, 0.0, 0.0)
     f = ctypes.c_float
-    assert L.defl_muon_step_batched(room, p(at), binding.F32, p(at), p(at), 1, 4, 4, binding.F32, f(0.1), f(0.9), 0, f(0.0), f(1.0), 1, 1, 1,
-                                    schedule, 1, ctypes.byref(o), None) == -1
+    assert L.defl_muon_step_scaled(room, p(at), binding.F32, p(at), p(at), 1, 4, 4, binding.F32, f(0.1), f(0.9), 0, f(0.0), f(1.0), 1, 1, 1,
+                                   schedule, 1, None, None, p(at + 2)) == -1
 
 
 def test_native_module_follows_its_torch_and_can_be_missing(libpath, monkeypatch, tmp_path):
@@ -190,3 +188,15 @@ def test_native_module_follows_its_torch_and_can_be_missing(libpath, monkeypatch
     with pytest.warns(UserWarning, match=r"no g\+\+"):
         assert build.build_native() is None
     assert len(ran) == 2 and not os.path.exists(target)
+
+
+def test_options_do_not_grow(tmp_path):
+    """defl_opts has no size field: a caller built against an earlier header passes one that ends with poly_terms, and no call may read on."""
+    import subprocess
+    from paper_2609_21102_b200 import binding
+    src, exe = tmp_path / "size.c", tmp_path / "size"
+    src.write_text('#include <stddef.h>\n#include <stdint.h>\n#include <stdio.h>\n#include "defl.h"\n'
+                   'int main(void) { printf("%zu %zu %zu\\n", sizeof(defl_opts), offsetof(defl_opts, poly_terms), _Alignof(defl_opts)); return 0; }\n')
+    subprocess.run(["gcc", "-I" + os.path.join(ROOT, "include"), str(src), "-o", str(exe)], check=True)
+    size, last, align = (int(x) for x in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split())
+    assert size == -(-(last + 4) // align) * align == ctypes.sizeof(binding.DeflOpts)

@@ -133,7 +133,7 @@ typedef struct defl_info {
  * DEFL_JACOBI_SWEEPS (sweep cap of the Jacobi core, default 40), DEFL_LANCZOS_FORM (the scale estimate of
  * DEFL_NORM_LANCZOS: 2 one launch per step, the form for n above 8192; else one launch for all of it),
  * DEFL_LANCZOS_HOLD (test hook: the waits of that launch run out), DEFL_MX4_HOLD (test hook: the waits of 4-bit products
- * of more than eight rows run out). */
+ * on the tensor cores run out). */
 int defl_create(defl_ctx** out, int device);
 int defl_destroy(defl_ctx* ctx);
 int defl_set_stream(defl_ctx* ctx, void* cuda_stream); /* cudaStream_t; NULL = default stream */
@@ -432,8 +432,8 @@ int defl_mx4_dequantize(defl_ctx* ctx, const defl_mx4* a, int b, int rows, int c
 
 /* D [b, M, N] = alpha A B^T with A [b, M, K] and B [b, N, K], or one B for all (b_shared != 0), of the same format; D row-major with row
  * stride ldd >= N and a batch stride of at least (M - 1) ldd + N, DEFL_BF16 or DEFL_F32, apart from A and B. Products are exact, sums are fp32, one rounding to bf16.
- * Up to eight rows of A (single tokens) the weights stream through integer products, else the tensor cores take the
- * scales with the codes (tcgen05 block-scaled products). A device-side wait that runs out is reported by
+ * Few rows of A (single tokens; up to eight where there are not too many weights) meet them in integer products, else the tensor cores
+ * take the scales with the codes (tcgen05 block-scaled products). A device-side wait that runs out is reported by
  * defl_device_wait_status. Errors as defl_mx4_quantize. */
 int defl_mx4_gemm(defl_ctx* ctx, const defl_mx4* A, const defl_mx4* B, int b, int M, int N, int K, int b_shared, int fmt, float alpha, void* D,
                   int64_t ldd, int64_t batch_stride, int out_dtype, void* work);

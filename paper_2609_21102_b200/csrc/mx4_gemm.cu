@@ -15,7 +15,7 @@
 // operands alone, 64 + 6 KB (nvfp4 + 12) for a 256 x 256 tile and 256 values of K: 207 us in mxfp4, 5.3 PFLOP/s, 224 in nvfp4. 8192 x 6400 x
 // 1600 to bf16, 47 and 52 us, moves 530 and 556 MB through L2, 105 of them D.
 //
-// mx4_row_kernel, for up to eight rows of A: the weights are read once at memory speed, each code becomes two bytes by table
+// mx4_row_kernel, for up to eight rows of A (by_rows below): the weights are read once at memory speed, each code becomes two bytes by table
 // lookup (prmt), four products at a time are integer dot products (dp4a), a block's sum meets its scales in fp32.
 #include "ctx.cuh"
 #include "mx4.cuh"
@@ -704,10 +704,32 @@ cudaError_t tc_start(const TcParams4& p, int grid, size_t smem, cudaStream_t st)
   return cudaLaunchKernelEx(&cfg, mx4_tc_kernel<FMT, PAIR, NSB>, p);
 }
 
+// Whether up to eight rows go through mx4_row_kernel. Its time grows with the rows it works out (M rounded up to a power of two) times the
+// weights, since every weight is looked up once and multiplied with each row; the tensor cores' form takes the same for any M here. us, row
+// kernel and tensor cores, mxfp4 with weights from HBM (nvfp4 is within a tenth of it, five to eight rows up to 1.3 times as long):
+//   N x K             M = 1        2           3, 4        5 to 8
+//   768 x 768         2.0  4.3   2.3  4.3    2.8  4.3    4.2  4.4
+//   1600 x 1600       2.8  6.3   3.5  6.3    4.4  6.3    7.1  6.3
+//   2048 x 2048       2.9  7.5   3.6  7.4    4.7  7.5    7.8  7.5     2^25 products in eight rows
+//   4096 x 2048       3.6  7.7   4.5  7.7    6.2  7.8   10.3  7.9     2^25 in four
+//   6400 x 1600       4.3  6.5   5.2  6.5    7.2  6.6   11.8  6.6
+//   4096 x 4096       5.0  9.7   6.9  9.7   10.5  9.7   18.3  9.7     2^25 in two
+//   12800 x 1600      6.6  7.6   8.8  7.8   12.4  7.6   21.4  7.8
+//   16384 x 4096     11.8 13.8  17.7 13.9   30.5 13.8   53.9 14.3     2^26 in one
+//   25600 x 1600     10.6  9.6  14.9 10.6   21.4 10.7   36.7 10.2
+//   20000 x 256       5.6  4.7   6.9  4.7    8.2  4.7   11.7  4.7     (a CTA for sixteen rows of B: short ones are mostly its start)
+bool by_rows(int b, int M, int N, int K) {
+  const int t = M <= 2 ? M : M <= 4 ? 4 : 8;
+  return M <= 8 && (long long)b * N <= 16384 && (long long)b * N * K * t <= (t == 1 ? 1ll << 26 : 1ll << 25);
+}
+
 template <int FMT, int T>
 cudaError_t row_start(const RowParams& p, int b, int num_sms, cudaStream_t st) {
-  // fewer rows than that would leave SMs without a CTA of sixteen of them
-  if (p.N >= num_sms * 4) return launch_kernel(mx4_row_kernel<FMT, T, 16>, dim3((unsigned)((p.N + 15) / 16), (unsigned)b), dim3(ROW_THREADS), 0, st, p);
+  // Sixteen lanes a row of B from four rows an SM on (long rows, which are worth more lanes: six), else half a CTA. us with 16 and with 128 lanes, mxfp4, one row of A and eight:
+  //   K 256    N 592   2.0  2.1   3.1  3.1     N 768   2.0  2.2   3.0  3.7     N 1024   2.0  2.4   3.1  4.1
+  //   K 1600   N 592   2.4  2.3   6.7  5.4     N 768   2.4  2.4   6.7  5.9     N 1024   2.4  2.5   6.7  7.6
+  //   K 6400   N 592   4.9  3.5  20.3 13.6     N 768   4.9  3.7  20.2 15.3     N 1024   4.9  4.2  20.3 19.8     N 1600   4.9  5.6  20.3 28.0
+  if (p.N >= num_sms * (p.K <= 1024 ? 4 : 6)) return launch_kernel(mx4_row_kernel<FMT, T, 16>, dim3((unsigned)((p.N + 15) / 16), (unsigned)b), dim3(ROW_THREADS), 0, st, p);
   return launch_kernel(mx4_row_kernel<FMT, T, ROW_THREADS / 2>, dim3((unsigned)((p.N + 1) / 2), (unsigned)b), dim3(ROW_THREADS), 0, st, p);
 }
 template <int FMT>
@@ -741,7 +763,7 @@ cudaError_t mx4_gemm_prepare() {
 
 Mx4Split mx4_gemm_split(int b, int M, int N, int K, int out_dtype, int num_sms) {
   Mx4Split r = {1, 0};
-  if (M <= 8) return r;
+  if (by_rows(b, M, N, K)) return r;
   Mx4Gemm g = {};
   g.b = b; g.M = M; g.N = N; g.K = K; g.out_dtype = out_dtype;
   const bool pair = M > 128;
@@ -758,7 +780,7 @@ Mx4Split mx4_gemm_split(int b, int M, int N, int K, int out_dtype, int num_sms) 
 }
 
 cudaError_t mx4_gemm_launch(const Mx4Gemm& g, cudaStream_t st, int* status, int num_sms, unsigned long long wait_ns, bool hold, long long* launches) {
-  if (g.M <= 8) {
+  if (by_rows(g.b, g.M, g.N, g.K)) {
     RowParams r;
     r.A = g.A; r.B = g.B; r.M = g.M; r.N = g.N; r.K = g.K; r.b_shared = g.b_shared;
     r.D = g.D; r.ldd = g.ldd; r.batch_d = g.batch_d; r.out_f32 = g.out_dtype == F32; r.alpha = g.alpha;

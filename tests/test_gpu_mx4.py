@@ -418,7 +418,7 @@ def test_bounded_wait_runs_out_and_is_reported(monkeypatch, ctx, fmt, shape):
     from paper_2609_21102_b200 import binding
     b, M, N, K = shape
     A, B = _mx(ctx, (b, M, K), 31, fmt), _mx(ctx, (b, N, K), 32, fmt)
-    few = A._replace(codes=A.codes[:, :8].contiguous(), scales=A.scales[:, :1].contiguous(), rows=8)
+    few = A._replace(codes=A.codes[:, :1].contiguous(), scales=A.scales[:, :1].contiguous(), rows=1)
     torch.cuda.synchronize()
     monkeypatch.setenv("DEFL_MX4_HOLD", "1")
     monkeypatch.setenv("DEFL_TC_WAIT_MS", "2")
@@ -427,7 +427,7 @@ def test_bounded_wait_runs_out_and_is_reported(monkeypatch, ctx, fmt, shape):
     held.defl_mx4_gemm(A, B)
     assert held.defl_device_wait_status(clear=False) == binding.ST_DEVICE_WAIT
     assert held.defl_device_wait_status() == binding.ST_DEVICE_WAIT and held.defl_device_wait_status() == 0
-    _check(held, held.defl_mx4_gemm(few, B, out_dtype=F32), few, B)            # (up to eight rows nothing waits)
+    _check(held, held.defl_mx4_gemm(few, B, out_dtype=F32), few, B)            # (a single row waits for nothing)
     assert held.defl_device_wait_status() == 0
     held.close()
     _check(ctx, ctx.defl_mx4_gemm(A, B, out_dtype=F32), A, B)
@@ -488,3 +488,26 @@ def test_mxfp4_rows_far_apart_in_size(ctx, rows, up):
     want = a.double() @ w.double().transpose(1, 2)
     assert torch.equal(ctx.defl_mx4_gemm(A, B, out_dtype=F32).double(), want)
     assert torch.equal(ctx.defl_mx4_gemm(B, A, out_dtype=F32).double(), want.transpose(1, 2))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("shape", [(1, 1, 16384, 96), (1, 1, 16385, 96), (1, 2, 8193, 2048), (1, 8, 2048, 2048), (1, 8, 2049, 2048), (1, 3, 9000, 1600),
+                                   (3, 5, 6000, 500), (40, 1, 410, 64), (1, 4, 700, 1000), (1, 7, 600, 1056), (1, 2, 890, 1056)])
+def test_few_rows_in_either_form(ctx, fmt, shape):
+    """Both sides of the rules that choose between the row kernel and the tensor cores, and its lanes: grid values with a six in every block, whose
+    sums are exact in any order (a multiple of 1/4 below 36 K < 2^22), and values of any size against fp64."""
+    b, M, N, K = shape
+    rng = np.random.default_rng(39)
+    vals = np.concatenate([mx4.GRID, -mx4.GRID])
+
+    def make(rows):
+        x = rng.choice(vals, (b, rows, K))
+        x[:, :, ::16] = 6.0
+        return torch.tensor(x, dtype=F32).cuda()
+    a, w = make(M), make(N)
+    D = ctx.defl_mx4_gemm(ctx.defl_mx4_quantize(a, fmt), ctx.defl_mx4_quantize(w, fmt), out_dtype=F32)
+    assert torch.equal(D.double(), a.double() @ w.double().transpose(1, 2))
+    A, B = _mx(ctx, (b, M, K), 40, fmt), _mx(ctx, (b, N, K), 41, fmt)
+    _check(ctx, ctx.defl_mx4_gemm(A, B), A, B)
+    assert ctx.defl_device_wait_status() == 0

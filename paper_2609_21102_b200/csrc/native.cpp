@@ -67,17 +67,23 @@ bool gradient(PyObject* o, Py_ssize_t i, int device, const void** x, int64_t* n,
   if (is_none(o)) return false;
   TORCH_CHECK_TYPE(THPVariable_Check(o), "gradient ", i, " must be a tensor");
   const Tensor& t = THPVariable_Unpack(o);
-  TORCH_CHECK_VALUE(t.is_cuda() && t.get_device() == device && t.is_contiguous(), "gradient ", i, " must be a contiguous tensor on cuda:", device);
+  TORCH_CHECK_VALUE(t.device() == c10::Device(c10::kCUDA, (c10::DeviceIndex)device) && t.is_contiguous(), "gradient ", i, " must be a contiguous tensor on cuda:", device);
   *type = code_of(t.scalar_type());
   TORCH_CHECK_TYPE(*type == DEFL_F32 || *type == DEFL_BF16, "gradient ", i, " must be float32 or bfloat16");
-  *x = t.data_ptr();
+  *x = t.const_data_ptr();
   *n = t.numel();
   return true;
 }
 
-// a tensor of an AdamWGroup is where it was when the group was made (386 parameters: 7 us for their two moments, 12 with scales)
-inline void in_place(const Tensor& t, const void* p, int64_t n, const char* what, Py_ssize_t i) {
-  TORCH_CHECK_VALUE(t.data_ptr() == p && t.numel() == n, what, " ", i, " has other memory than when its AdamWGroup was made");
+// A tensor of an AdamWGroup is where it was when the group was made. (386 parameters with their moments are some thousand tensors a call, each
+// behind three pointers: the address is put together here from what it is made of, and the message out of the way.)
+[[noreturn]] __attribute__((noinline, cold)) void moved(const char* what, Py_ssize_t i) {
+  TORCH_CHECK_VALUE(false, what, " ", i, " has other memory than when its AdamWGroup was made");
+}
+inline const void* address_of(PyObject* o) {
+  const c10::TensorImpl* im = THPVariable_Unpack(o).unsafeGetTensorImpl();
+  const c10::StorageImpl* storage = im->unsafe_storage().unsafeGetStorageImpl();
+  return storage ? static_cast<const char*>(storage->data()) + im->storage_offset() * (int64_t)im->itemsize() : nullptr;
 }
 
 // adamw_step(handle, device, table address, params, grads, lr, step, beta1, beta2, eps, weight_decay, grad_scale, stochastic, seed[, others]) -> code
@@ -100,36 +106,30 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   o.seed = PyLong_AsUnsignedLongLongMask(a[13]);
   if (PyErr_Occurred()) throw python_error();
   // (a copy for this call, with its gradients: the group's table is shared by all)
-  std::vector<defl_adamw_tensor> table(held, held + count);
-  if (nargs == 15) {
-    const Sequence others(a[14]);
-    Py_ssize_t at = 0;
-    auto next = [&](const void* p, int64_t n, const char* what, Py_ssize_t i) {
-      TORCH_CHECK_VALUE(at < others.size(), "tensors of the AdamWGroup are missing");
-      // (the group holds nothing but tensors. 386 to 1544 of them, each behind three pointers: those of a later one are asked for now)
-      if (at + 8 < others.size()) __builtin_prefetch(THPVariable_Unpack(others[at + 8]).unsafeGetTensorImpl());
-      if (at + 4 < others.size()) __builtin_prefetch(THPVariable_Unpack(others[at + 4]).unsafeGetTensorImpl()->unsafe_storage().unsafeGetStorageImpl());
-      in_place(THPVariable_Unpack(others[at++]), p, n, what, i);
-    };
-    for (Py_ssize_t i = 0; i < count; ++i) {
-      const defl_adamw_tensor& t = table[i];
-      const int64_t blocks = (t.n + 255) / 256;
-      if (t.n == 0) continue;
-      next(t.m, t.n, "first moment", i);
-      next(t.v, t.n, "second moment", i);
-      if (t.state_bits == 8) {
-        next(t.m_scale, blocks, "first moment's scales", i);
-        next(t.v_scale, blocks, "second moment's scales", i);
-      }
-      if (t.copy) next(t.copy, t.n, "copy", i);
-    }
-  }
+  std::vector<defl_adamw_tensor> table;
+  table.reserve((size_t)count);
+  std::optional<Sequence> others;                            // (a group's own: nothing but tensors)
+  if (nargs == 15) others.emplace(a[14]);
+  Py_ssize_t at = 0;
   for (Py_ssize_t i = 0; i < count; ++i) {
+    table.push_back(held[i]);
+    defl_adamw_tensor& t = table.back();
+    const Tensor& p = tensor(params[i], "a parameter");
+    if (p.const_data_ptr() != t.p || p.numel() != t.n) moved("parameter", i);
+    if (others && t.n > 0) {
+      TORCH_CHECK_VALUE(at + 2 + (t.state_bits == 8 ? 2 : 0) + (t.copy ? 1 : 0) <= others->size(), "tensors of the AdamWGroup are missing");
+      if (address_of((*others)[at++]) != t.m) moved("first moment", i);
+      if (address_of((*others)[at++]) != t.v) moved("second moment", i);
+      if (t.state_bits == 8) {
+        if (address_of((*others)[at++]) != t.m_scale) moved("first moment's scales", i);
+        if (address_of((*others)[at++]) != t.v_scale) moved("second moment's scales", i);
+      }
+      if (t.copy && address_of((*others)[at++]) != t.copy) moved("copy", i);
+    }
     int64_t n = 0;
-    in_place(tensor(params[i], "a parameter"), table[i].p, table[i].n, "parameter", i);
-    table[i].g = nullptr;
-    if (!gradient(grads[i], i, device, &table[i].g, &n, &table[i].g_dtype)) continue;
-    TORCH_CHECK_VALUE(n == table[i].n, "gradient ", i, " has ", n, " elements, its parameter ", table[i].n);
+    t.g = nullptr;
+    if (!gradient(grads[i], i, device, &t.g, &n, &t.g_dtype)) continue;
+    TORCH_CHECK_VALUE(n == t.n, "gradient ", i, " has ", n, " elements, its parameter ", t.n);
   }
   int rc;
   {

@@ -370,7 +370,8 @@ int defl_adamw_step(defl_ctx* ctx, const defl_adamw_tensor* tensors, int count, 
 /* Global norm of a list of gradients and what follows from it, without the host:
  *   out[0] = sqrt(sum of all squares)            out[1] = min(1, max_norm / (out[0] + 1e-6)), 1 if max_norm <= 0
  * A norm that is Inf or NaN makes out[1] zero (defl_adamw_step then leaves its step out) and *step stays; else *step, if
- * given, is advanced by one: the number of the step that follows. Sums are in fp64, in an order that only the sizes decide.
+ * given, is advanced by one: the number of the step that follows. Eight squares at a time are summed in fp32 (where that sum leaves
+ * 1e-30 .. 1e38, in fp64), those sums in fp64, in an order that only the sizes decide.
  *   tensors  host, `count` of them (n = 0 is skipped);  out  device, [2] fp32;  step  device, NULL or one int64
  *   work     device, defl_grad_norm_work_bytes(count) bytes, 8-byte aligned, of this call alone until it is through: calls that
  *            may run at the same time (two streams, two captured graphs) need one each
@@ -427,7 +428,8 @@ int defl_mx4_quantize(defl_ctx* ctx, const void* X, int dtype, int b, int rows, 
                       const defl_mx4* by_rows, const defl_mx4* by_cols, void* work);
 
 /* out [b, rows, cols] contiguous, DEFL_BF16 or DEFL_F32: the values that the codes stand for, code * scale rounded once (both types
- * hold them exactly while the matrix's scale is a power of two). */
+ * hold them exactly while the matrix's scale is a power of two, except that a value that rounds to 2^128, which takes one
+ * above 3.4 * 2^126 in magnitude, comes back infinite). */
 int defl_mx4_dequantize(defl_ctx* ctx, const defl_mx4* a, int b, int rows, int cols, int fmt, void* out, int dtype);
 
 /* D [b, M, N] = alpha A B^T with A [b, M, K] and B [b, N, K], or one B for all (b_shared != 0), of the same format; D row-major with row

@@ -611,7 +611,9 @@ int defl_mx4_quantize(defl_ctx* c, const void* X, int dtype, int b, int rows, in
   const unsigned es = (unsigned)dtype_size(dtype);
   if (!on(X, es)) return DEFL_ERR_ARG;
   if (rows > DEFL_MX4_MAX_SIDE || cols > DEFL_MX4_MAX_SIDE || b > 65535) return DEFL_ERR_RANK;
-  const bool scan = (long long)rows * cols <= DEFL_MX4_SCAN_MOST;    // every CTA finds the largest magnitude by itself
+  // nvfp4: up to this size every CTA finds the largest magnitude by itself, which saves a launch. us that way and with the launch, blocks along the
+  // rows: bf16 8192 values 2.9 5.0, 32000 4.2 4.9, 64000 5.7 4.9, 131072 8.1 4.3; fp32 8192 3.7 5.4, 32000 5.6 5.5, 64000 7.8 5.5
+  const bool scan = (long long)rows * cols <= DEFL_MX4_SCAN_MOST;
   static_assert(DEFL_MX4_SCAN_MOST <= 0x7fffffff, "the kernel counts these values in 32 bits");
   if (fmt == DEFL_NVFP4 && !scan && (!work || !on(work, 4))) return DEFL_ERR_ARG;
   DeviceScope scope(c->device);

@@ -15,8 +15,11 @@ namespace {
 
 constexpr int OPT_THREADS = 256;
 constexpr int CHUNK = 2048;                       // elements of one CTA's trip: 8 a thread, a block of 256 a warp
-constexpr int ADAM_CAP = 438, ADAM_CAP_SMALL = 48, ADAM_CAP_MID = 160;   // tensors a launch: 438 x 72 bytes fill the 32,764 bytes of parameters
-constexpr int NORM_CAP = 1300, NORM_CAP_MID = 440, NORM_CAP_SMALL = 48;      // (a launch copies its parameters whole)
+// Tensors a launch. The largest tables stay within the 32,764 bytes that a launch's parameters may take (31.7 and 31.2 KB); a launch copies its
+// parameters whole, which the smaller ones save (us on the host with the largest table, the middle one and the smallest; graphs do not care:
+// AdamW 4 tensors 4.7 3.8 3.3, 48 tensors 6.6 5.6 5.2, 160 tensors 10.8 9.8; norm 4 tensors 6.9 5.8 5.1, 48 7.5 6.4 5.9, 386 12.1 10.8).
+constexpr int ADAM_CAP = 438, ADAM_CAP_SMALL = 48, ADAM_CAP_MID = 160;
+constexpr int NORM_CAP = 1300, NORM_CAP_MID = 440, NORM_CAP_SMALL = 48;
 constexpr int NORM_BLOCKS = 592;                  // four CTAs on each of 148 SMs
 constexpr int NORM_CHUNK = 4 * CHUNK;
 

@@ -269,7 +269,7 @@ class Context:
     """defl_ctx bound to one CUDA device; work is enqueued on torch's current stream at call time."""
 
     def __init__(self, device=0):
-        self.device = torch.device("cuda", device) if not isinstance(device, torch.device) else device
+        self.device = torch.device("cuda", (device.index or 0) if isinstance(device, torch.device) else device)
         h = ctypes.c_void_p()
         rc = lib().defl_create(ctypes.byref(h), self.device.index or 0)
         if rc != 0:

@@ -345,6 +345,21 @@ def test_a_moment_that_has_moved(ctx, which):
 
 
 @pytest.mark.gpu
+def test_context_of_a_device_without_a_number():
+    """torch.device("cuda") is the first device, as the tensors that were made on it say; they are not refused."""
+    from paper_2609_21102_b200 import binding
+    c = binding.Context(torch.device("cuda"))
+    f = lambda: torch.ones(300, device="cuda")  # noqa: E731
+    p, g = f(), f()
+    clip = c.defl_grad_norm([g], 1.0)
+    c.defl_adamw_step(binding.AdamWGroup([p], [f()], [f()]), [g], torch.full((1,), LR, device="cuda"), 1, grad_scale=clip)
+    W, G = torch.randn(1, 32, 48, device="cuda"), torch.randn(1, 32, 48, device="cuda")
+    c.defl_muon_step_batched(W, torch.zeros_like(W), G, LR, 0.9, 2, 2, 1, [list(binding.MUON_QUINTIC)] * 2, grad_scale=clip)
+    assert torch.all(p < 1) and torch.isfinite(W).all()
+    c.close()
+
+
+@pytest.mark.gpu
 def test_smallest_eps(ctx):
     """An eps below fp32's normal numbers is zero; where both moments are, the quotient is then NaN, as 0 / 0 is."""
     from paper_2609_21102_b200 import binding

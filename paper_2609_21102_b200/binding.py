@@ -538,14 +538,14 @@ class Context:
     def defl_mx4_dequantize(self, q, dtype=torch.bfloat16):
         """The values [b, rows, cols] that an Mx4 stands for, in bfloat16 or float32."""
         return self._result(_native().mx4_dequantize(self._handle, self._index, q.codes, q.scales, q.scale, q.fmt, q.rows, q.cols,
-                                                     _DTYPE_CODE[dtype]))
+                                                     _DTYPE_CODE.get(dtype, -1)))
 
     def defl_mx4_gemm(self, A, B, out_dtype=torch.bfloat16, out=None, alpha=1.0):
         """alpha A B^T [b, M, N] of two Mx4 of one format that agree in cols, in bfloat16 or float32; a B of batch 1 serves every A."""
         if A.fmt != B.fmt or A.cols != B.cols:
             raise ValueError("A and B must agree in format, columns and batch")
         return self._result(_native().mx4_gemm(self._handle, self._index, A.codes, A.scales, A.scale, B.codes, B.scales, B.scale,
-                                               A.fmt, A.rows, B.rows, A.cols, out, _DTYPE_CODE[out_dtype], alpha))
+                                               A.fmt, A.rows, B.rows, A.cols, out, _DTYPE_CODE.get(out_dtype, -1), alpha))
 
     def defl_fill_gaussian(self, dst, seed):
         _dev(dst, "dst")

@@ -511,3 +511,15 @@ def test_few_rows_in_either_form(ctx, fmt, shape):
     A, B = _mx(ctx, (b, M, K), 40, fmt), _mx(ctx, (b, N, K), 41, fmt)
     _check(ctx, ctx.defl_mx4_gemm(A, B), A, B)
     assert ctx.defl_device_wait_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float64, torch.float16, torch.int8, torch.float8_e4m3fn, None])
+def test_result_types_that_there_are_not(ctx, dtype):
+    """All are refused as arguments, those that the library has no number for too."""
+    from paper_2609_21102_b200 import binding
+    q = ctx.defl_mx4_quantize(torch.ones(1, 4, 32, device="cuda"))
+    for call in (lambda: ctx.defl_mx4_dequantize(q, dtype), lambda: ctx.defl_mx4_gemm(q, q, out_dtype=dtype)):
+        with pytest.raises(binding.DeflError) as e:
+            call()
+        assert e.value.code == -1

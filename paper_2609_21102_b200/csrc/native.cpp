@@ -43,9 +43,15 @@ void use_stream(defl_ctx* c, int device) { defl_set_stream(c, c10::cuda::getCurr
 // on one context take turns.
 std::mutex& lock_of(defl_ctx* c) {
   static std::mutex all;
-  static auto* each = new std::map<defl_ctx*, std::mutex>;
-  const std::lock_guard<std::mutex> one(all);
-  return (*each)[c];
+  static auto* each = new std::map<defl_ctx*, std::mutex>;   // (never taken apart: a later context at an old address has the old one's)
+  static thread_local defl_ctx* last = nullptr;
+  static thread_local std::mutex* lock = nullptr;
+  if (!lock || last != c) {
+    const std::lock_guard<std::mutex> one(all);
+    lock = &(*each)[c];
+    last = c;
+  }
+  return *lock;
 }
 struct Unlocked {
   PyThreadState* const state;

@@ -212,7 +212,8 @@ class AdamWGroup:
     sizes, all float32 or, in 8 bits, float8_e4m3fn with float32 scales [ceil(n / 256)] (the second moment is held as its
     root); optional bfloat16 copies of the parameters. The group keeps the tensors' memory alive; no two of them may overlap.
     A tensor of the group that has been given other memory since (p.data = ..., .to(...)) is refused: it needs a new group, and so
-    do other tensors in its place (the group's lists are tuples)."""
+    do other tensors in its place (the group's lists are tuples). Making one takes some milliseconds where a step takes microseconds (386
+    parameters: 2.4 ms, with 8-bit moments 4.7)."""
     params, exp_avg, exp_avg_sq, avg_scale, root_scale, copies = (property(lambda self, i=i: self._lists[i]) for i in range(6))
 
     def __init__(self, params, exp_avg, exp_avg_sq, avg_scale=None, root_scale=None, copies=None):

@@ -11,9 +11,11 @@
 // Tensor memory: 512 columns = two accumulators and four sets of scales (24 columns each, nvfp4 48). Two accumulators of 256 columns
 // leave no room for that, so they overlap (by 96 and 192 columns); the read-out takes those first and says so, and the next tile's
 // products wait for that much only. (Copies run on meanwhile, and products are twice as fast as copies.)
-// What bounds it: what L2 delivers to the whole chip, 11 TB/s (5500 to 6000 bytes a cycle at 1.9 GHz). 8192 x 8192 x 8192 takes that for
-// operands alone, 64 + 6 KB (nvfp4 + 12) for a 256 x 256 tile and 256 values of K: 207 us in mxfp4, 5.3 PFLOP/s, 224 in nvfp4. 8192 x 6400 x
-// 1600 to bf16, 47 and 52 us, moves 530 and 556 MB through L2, 105 of them D.
+// What bounds it. 8192 x 8192 x 8192: what arrives from L2 at all SMs together, 11 TB/s (5500 to 6000 bytes a cycle at 1.9 GHz), 64 + 6 KB (nvfp4
+// + 12) for a 256 x 256 tile and 256 values of K: 206 us in mxfp4, 5.3 PFLOP/s, 226 in nvfp4. 8192 x 6400 x 1600 to bf16, 47 and 52 us, moves
+// 530 and 556 MB through L2, 105 of them D: a CTA fetches its 128 rows of A again for each of 25 columns of tiles, half of what it reads. 8192 x
+// 1600 x 6400 and 6400 x 1600 x 8192, 47 to 49 and 45 to 47: the last wave (3.03 and 2.36 waves of 256-wide tiles over 74 pairs, taken as four of
+// 192 and as three). In nvfp4 the tensor pipe is busy 34, 36 and 37 % of these three, L2's slices 37, 32 and 29 %.
 //
 // mx4_row_kernel, for up to eight rows of A (by_rows below): the weights are read once at memory speed, each code becomes two bytes by table
 // lookup (prmt), four products at a time are integer dot products (dp4a), a block's sum meets its scales in fp32.

@@ -298,10 +298,11 @@ __device__ __forceinline__ void adam_block(const AdamTensor& t, const AdamHyper&
 }
 
 // Bytes an element with fp32 weights and bf16 gradients: 26 with 32-bit moments, 14.1 with 8-bit ones; what HBM can bring of
-// that in a second leaves 150 and 77 instructions an element. 80M elements on a B200: 312 us with 32-bit moments (6.7 TB/s: bound by HBM), with
-// 8-bit ones 194 to nearest and 230 with random bits, which are bound by the issue of instructions (about 90 an element, 84 % of the slots
-// taken): the generator's two 64-bit products and shifts take 28 us of that, the exact square root 14. Two blocks a trip take registers that spill
-// (276), three CTAs an SM leave too little to hide (255).
+// that in a second leaves 150 and 77 instructions an element. 80M elements on a B200: 313 us with 32-bit moments (6.7 TB/s: bound by HBM; bf16
+// weights 264, to nearest or random), with 8-bit ones 191 to nearest and 231 with random bits, which are bound by the issue of instructions (84
+// an element, 82 % of the slots taken; under the power cap of half a second without a pause 257): the generator's two 64-bit products and shifts
+// take 28 us of that, the exact square root 14. Two blocks a trip take registers that spill (276; as it is, 16 bytes do), three CTAs an SM
+// leave too little to hide (255).
 template <typename P, typename G, bool EIGHT, bool SR, int CAP>
 __global__ void __launch_bounds__(OPT_THREADS, 4) adamw_kernel(const __grid_constant__ AdamTable<CAP> tb) {
   __shared__ Scalars sc;
@@ -383,7 +384,8 @@ __device__ __forceinline__ double block_sum(double acc, double* part) {
   return d;
 }
 
-// Reads 2 or 4 bytes an element and writes nothing: bound by HBM, so four loads of a thread are in flight.
+// Reads 2 or 4 bytes an element and writes nothing, so four loads of a thread are in flight. bf16: 80M elements 44 us, the 1.47G of a model 717:
+// 4.1 of the 6.5 TB/s that HBM brings; what keeps it there has not been taken apart.
 template <int CAP>
 __global__ void __launch_bounds__(OPT_THREADS) grad_norm_kernel(const __grid_constant__ NormTable<CAP> tb) {
   __shared__ double part[OPT_THREADS / 32];

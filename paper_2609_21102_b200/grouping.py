@@ -80,7 +80,9 @@ def optimizer_step_groups(ctx, weights, momenta, grads, lr, mu, window, oversamp
     on the rest, a binding.AdamWGroup with one gradient per tensor (None: left alone). The global norm is taken over all
     gradients together; with max_norm > 0 its factor scales both kinds. rest_step is an int64 CUDA tensor [1], the number of
     AdamW steps taken so far: it is advanced on the device. A norm that is not finite leaves the rest and the counter as they are,
-    and the matrices take a step along their momentum without the gradient. `adamw`: further arguments of defl_adamw_step.
+    and the matrices take a step along their momentum without the gradient: the factor is on the device, the launches of a Muon step do
+    not depend on it, and its momentum rule has a meaning for a gradient of zero. (Who wants such a step left out altogether reads the factor
+    of defl_grad_norm first, which waits for it.) `adamw`: further arguments of defl_adamw_step.
     Nothing waits; returns the tensor (norm, factor). A missing gradient under nesterov=True and a list of gradients of the wrong
     length are refused before the counter, the weights or the moments change."""
     rest_grads = list(rest_grads)

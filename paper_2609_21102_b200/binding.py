@@ -255,12 +255,17 @@ class AdamWGroup:
             ptr = lambda t: t.data_ptr() if t is not None else 0  # noqa: E731
             self.table[i] = (ptr(p), 0, ptr(m), ptr(v), ptr(ms) if eight else 0, ptr(vs) if eight else 0, ptr(c), n, _dtype_code(p), F32,
                              8 if eight else 32)
-        self._others = tuple(self._others)
+        self._others, self._held = tuple(self._others), None
         self.address, self.count = self.table.ctypes.data, count
         spans.sort()
         for a, b in zip(spans, spans[1:]):
             if b[0] < a[1]:
                 raise ValueError("%s and %s overlap" % (a[2], b[2]))
+
+    def _hold(self):
+        if self._held is None:
+            self._held = _native().adamw_hold(self.address, self.count, self._others)
+        return self._held
 
     def __reduce_ex__(self, protocol):
         raise TypeError("an AdamWGroup holds addresses and is not copied or pickled: make one of the copied tensors")
@@ -512,7 +517,7 @@ class Context:
         if group.device is not None and group.device != self.device:
             raise ValueError("the group's tensors are on %s, the context is on %s" % (group.device, self.device))
         self._check(_native().adamw_step(self._handle, self._index, group.address, group.params, grads, lr, step, betas[0], betas[1], eps,
-                                         weight_decay, grad_scale, stochastic, seed, group._others))
+                                         weight_decay, grad_scale, stochastic, seed, group._held or group._hold()))
 
     def _scalar(self, t, dtype, count, what):
         if t.device != self.device or t.dtype != dtype or t.numel() != count or not t.is_contiguous():

@@ -81,19 +81,82 @@ bool gradient(PyObject* o, Py_ssize_t i, int device, const void** x, int64_t* n,
   return true;
 }
 
-// A tensor of an AdamWGroup is where it was when the group was made. (386 parameters with their moments are some thousand tensors a call, each
-// behind three pointers: the address is put together here from what it is made of, and the message out of the way.)
 [[noreturn]] __attribute__((noinline, cold)) void moved(const char* what, Py_ssize_t i) {
   TORCH_CHECK_VALUE(false, what, " ", i, " has other memory than when its AdamWGroup was made");
 }
-inline const void* address_of(PyObject* o) {
-  const c10::TensorImpl* im = THPVariable_Unpack(o).unsafeGetTensorImpl();
-  const c10::StorageImpl* storage = im->unsafe_storage().unsafeGetStorageImpl();
-  return storage ? static_cast<const char*>(storage->data()) + im->storage_offset() * (int64_t)im->itemsize() : nullptr;
+
+// Where the tensors were that an AdamWGroup's table points to beside the parameters, looked at again in every call: each tensor's storage, its place in
+// it unless it is all of it (a view of that has the same memory), and each storage's address. (386 parameters have 772 moments, or 1544 tensors with
+// scales. What a look costs is the lines of memory it touches, so those of Python's objects and most of those of the tensors are left out.)
+struct Held {
+  struct Item { const c10::TensorImpl* tensor; const c10::StorageImpl* storage; int64_t offset; };      // offset -1: all of its storage
+  struct Place { const char* what; Py_ssize_t i; };
+  std::vector<Item> items;
+  std::vector<Place> places;                                 // of the items
+  std::vector<std::pair<const c10::StorageImpl*, const void*>> memory;
+  std::vector<size_t> first;                                 // the first item of each storage
+  std::vector<Tensor> tensors;                               // keep what the pointers point to
+  std::vector<c10::Storage> storages;
+
+  void add(const Tensor& t, const void* p, const char* what, Py_ssize_t i, std::map<const c10::StorageImpl*, size_t>& known) {
+    if (t.data_ptr() != p) moved(what, i);
+    const c10::StorageImpl* s = t.storage().unsafeGetStorageImpl();
+    if (known.emplace(s, memory.size()).second) {
+      memory.emplace_back(s, s->data());
+      first.push_back(items.size());
+      storages.push_back(t.storage());
+    }
+    const bool all = t.storage_offset() == 0 && (size_t)t.numel() * t.element_size() == s->nbytes();
+    items.push_back({t.unsafeGetTensorImpl(), s, all ? -1 : t.storage_offset()});
+    places.push_back({what, i});
+    tensors.push_back(t);
+  }
+  void check() const {
+    for (size_t k = 0; k < items.size(); ++k) {
+      const Item& x = items[k];
+      if (x.tensor->unsafe_storage().unsafeGetStorageImpl() != x.storage || (x.offset >= 0 && x.tensor->storage_offset() != x.offset))
+        moved(places[k].what, places[k].i);
+    }
+    for (size_t k = 0; k < memory.size(); ++k)
+      if (memory[k].first->data() != memory[k].second) moved(places[first[k]].what, places[first[k]].i);
+  }
+};
+
+// adamw_hold(table address, count, others) -> what adamw_step looks at. others: for each parameter that is not empty its moments, their scales in 8 bits, its
+// copy if it has one
+PyObject* adamw_hold(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK(nargs == 3, "adamw_hold takes 3 arguments");
+  const defl_adamw_tensor* table = reinterpret_cast<const defl_adamw_tensor*>(PyLong_AsVoidPtr(a[0]));
+  const Py_ssize_t count = PyLong_AsSsize_t(a[1]);
+  if (PyErr_Occurred()) throw python_error();
+  const Sequence others(a[2]);
+  auto held = std::make_unique<Held>();
+  std::map<const c10::StorageImpl*, size_t> known;
+  Py_ssize_t at = 0;
+  auto next = [&](const void* p, const char* what, Py_ssize_t i) {
+    TORCH_CHECK_VALUE(at < others.size(), "tensors of the AdamWGroup are missing");
+    held->add(tensor(others[at++], what), p, what, i, known);
+  };
+  for (Py_ssize_t i = 0; i < count; ++i) {
+    const defl_adamw_tensor& t = table[i];
+    if (t.n == 0) continue;
+    next(t.m, "first moment", i);
+    next(t.v, "second moment", i);
+    if (t.state_bits == 8) {
+      next(t.m_scale, "first moment's scales", i);
+      next(t.v_scale, "second moment's scales", i);
+    }
+    if (t.copy) next(t.copy, "copy", i);
+  }
+  PyObject* made = PyCapsule_New(held.get(), "Held", [](PyObject* o) { delete static_cast<Held*>(PyCapsule_GetPointer(o, "Held")); });
+  if (!made) throw python_error();
+  held.release();
+  return made;
+  END_HANDLE_TH_ERRORS
 }
 
-// adamw_step(handle, device, table address, params, grads, lr, step, beta1, beta2, eps, weight_decay, grad_scale, stochastic, seed[, others]) -> code
-// others: for each parameter that is not empty its moments, their scales in 8 bits, its copy if it has one
+// adamw_step(handle, device, table address, params, grads, lr, step, beta1, beta2, eps, weight_decay, grad_scale, stochastic, seed[, adamw_hold's]) -> code
 PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
   TORCH_CHECK(nargs == 14 || nargs == 15, "adamw_step takes 14 or 15 arguments");
@@ -114,24 +177,16 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   // (a copy for this call, with its gradients: the group's table is shared by all)
   std::vector<defl_adamw_tensor> table;
   table.reserve((size_t)count);
-  std::optional<Sequence> others;                            // (a group's own: nothing but tensors)
-  if (nargs == 15) others.emplace(a[14]);
-  Py_ssize_t at = 0;
+  if (nargs == 15) {
+    const Held* rest = static_cast<const Held*>(PyCapsule_GetPointer(a[14], "Held"));
+    if (!rest) throw python_error();
+    rest->check();
+  }
   for (Py_ssize_t i = 0; i < count; ++i) {
     table.push_back(held[i]);
     defl_adamw_tensor& t = table.back();
     const Tensor& p = tensor(params[i], "a parameter");
     if (p.const_data_ptr() != t.p || p.numel() != t.n) moved("parameter", i);
-    if (others && t.n > 0) {
-      TORCH_CHECK_VALUE(at + 2 + (t.state_bits == 8 ? 2 : 0) + (t.copy ? 1 : 0) <= others->size(), "tensors of the AdamWGroup are missing");
-      if (address_of((*others)[at++]) != t.m) moved("first moment", i);
-      if (address_of((*others)[at++]) != t.v) moved("second moment", i);
-      if (t.state_bits == 8) {
-        if (address_of((*others)[at++]) != t.m_scale) moved("first moment's scales", i);
-        if (address_of((*others)[at++]) != t.v_scale) moved("second moment's scales", i);
-      }
-      if (t.copy && address_of((*others)[at++]) != t.copy) moved("copy", i);
-    }
     int64_t n = 0;
     t.g = nullptr;
     if (!gradient(grads[i], i, device, &t.g, &n, &t.g_dtype)) continue;
@@ -354,7 +409,8 @@ PyObject* mx4_gemm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
-PyMethodDef methods[] = {{"adamw_step", (PyCFunction)(void (*)(void))adamw_step, METH_FASTCALL, nullptr},
+PyMethodDef methods[] = {{"adamw_hold", (PyCFunction)(void (*)(void))adamw_hold, METH_FASTCALL, nullptr},
+                         {"adamw_step", (PyCFunction)(void (*)(void))adamw_step, METH_FASTCALL, nullptr},
                          {"grad_norm", (PyCFunction)(void (*)(void))grad_norm, METH_FASTCALL, nullptr},
                          {"mx4_quantize", (PyCFunction)(void (*)(void))mx4_quantize, METH_FASTCALL, nullptr},
                          {"mx4_dequantize", (PyCFunction)(void (*)(void))mx4_dequantize, METH_FASTCALL, nullptr},

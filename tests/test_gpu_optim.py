@@ -345,6 +345,40 @@ def test_a_moment_that_has_moved(ctx, which):
 
 
 @pytest.mark.gpu
+def test_moments_that_share_a_buffer(ctx):
+    """Views of one buffer: another place in it, and a buffer that was given other memory itself, are refused; a view of all of a tensor's own
+    memory is that memory. What moved before the first step is seen by it."""
+    from paper_2609_21102_b200 import binding
+    f = lambda n: torch.zeros(n, device="cuda")  # noqa: E731
+    flat, p, g = f(1000), f(100), torch.ones(100, device="cuda")
+    m, v = flat[:100], flat[100:200]
+    group = binding.AdamWGroup([p], [m], [v])
+    m.data = flat[200:300]
+    with pytest.raises(ValueError, match="first moment 0"):
+        ctx.defl_adamw_step(group, [g], LR, 1)               # (the first one)
+    m.data = flat[:100]
+    ctx.defl_adamw_step(group, [g], LR, 1)
+    assert torch.all(m > 0)
+    v.data = flat[300:400]
+    held = p.clone()
+    with pytest.raises(ValueError, match="second moment 0"):
+        ctx.defl_adamw_step(group, [g], LR, 2)
+    v.data = flat[100:200]
+    ctx.defl_adamw_step(group, [g], LR, 2)
+    assert not torch.equal(p, held)
+    held.copy_(p)
+    flat.untyped_storage().resize_(4 * 2000)
+    with pytest.raises(ValueError, match="moment 0"):
+        ctx.defl_adamw_step(group, [g], LR, 3)
+    assert torch.equal(p, held)
+    own = f(100)
+    group = binding.AdamWGroup([p], [own], [f(100)])
+    own.data = own.data[:50]
+    ctx.defl_adamw_step(group, [g], LR, 1)
+    assert torch.all(own > 0)
+
+
+@pytest.mark.gpu
 def test_context_of_a_device_without_a_number():
     """torch.device("cuda") is the first device, as the tensors that were made on it say; they are not refused."""
     from paper_2609_21102_b200 import binding

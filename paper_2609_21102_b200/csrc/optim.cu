@@ -508,6 +508,20 @@ int defl_adamw_step(defl_ctx* c, const defl_adamw_tensor* t, int count, const de
   if (!on(o->step_dev, 8) || !on(o->lr_dev, 4) || !on(o->grad_scale, 4)) return DEFL_ERR_ARG;
   unsigned long long total = 0;
   unsigned int present = 0;                       // the combinations of types that the list holds
+  AdamTable<ADAM_CAP> tb;
+  auto start = [&] { tb.count = 0; tb.chunks = 0; };
+  auto put = [&](int i) {
+    const defl_adamw_tensor& x = t[i];
+    AdamTensor& d = tb.t[tb.count++];
+    d.p = x.p; d.g = x.g; d.m = x.m; d.v = x.v; d.ms = x.m_scale; d.vs = x.v_scale; d.copy = x.copy; d.n = x.n;
+    d.first = tb.chunks;
+    const bool aligned = on16(x.p) && on16(x.g) && on16(x.m) && on16(x.v) && on16(x.copy);
+    d.index = (int)((unsigned int)i | (aligned ? 0x80000000u : 0u));
+    tb.chunks += (unsigned int)((x.n + CHUNK - 1) / CHUNK);
+  };
+  // the usual list, of one combination of types and no longer than a table, is put down while it is looked through
+  bool whole = true;
+  start();
   for (int i = 0; i < count; ++i) {
     const defl_adamw_tensor& x = t[i];
     if (x.n < 0 || x.n > MAX_ELEMENTS) return DEFL_ERR_ARG;
@@ -519,12 +533,13 @@ int defl_adamw_step(defl_ctx* c, const defl_adamw_tensor* t, int count, const de
     if (!on(x.p, (unsigned)dtype_size(x.p_dtype)) || !on(x.g, (unsigned)dtype_size(x.g_dtype)) || !on(x.copy, 2)) return DEFL_ERR_ARG;
     if (x.state_bits == 32 && (!on(x.m, 4) || !on(x.v, 4))) return DEFL_ERR_ARG;
     present |= 1u << type_class(x);
+    whole = whole && (present & (present - 1)) == 0 && tb.count < ADAM_CAP;
+    if (whole) put(i);
     total += (unsigned long long)((x.n + CHUNK - 1) / CHUNK);
   }
   if (total > 0x7fffffffull) return DEFL_ERR_RANK;
   DeviceScope scope(c->device);
   c->err[0] = 0;
-  AdamTable<ADAM_CAP> tb;
   AdamHyper& h = tb.h;
   h.beta1 = o->beta1; h.beta2 = o->beta2; h.lr = o->lr; h.decay = o->weight_decay;
   h.step = o->step; h.step_dev = reinterpret_cast<const long long*>(o->step_dev); h.lr_dev = o->lr_dev; h.grad_scale = o->grad_scale;
@@ -542,17 +557,12 @@ int defl_adamw_step(defl_ctx* c, const defl_adamw_tensor* t, int count, const de
   for (int cls = 0; cls < 8; ++cls) {
     if (!(present >> cls & 1u)) continue;
     for (int i = 0; i < count;) {
-      tb.count = 0;
-      tb.chunks = 0;
-      for (; i < count && tb.count < ADAM_CAP; ++i) {
-        const defl_adamw_tensor& x = t[i];
-        if (x.n == 0 || !x.g || type_class(x) != cls) continue;
-        AdamTensor& d = tb.t[tb.count++];
-        d.p = x.p; d.g = x.g; d.m = x.m; d.v = x.v; d.ms = x.m_scale; d.vs = x.v_scale; d.copy = x.copy; d.n = x.n;
-        d.first = tb.chunks;
-        const bool aligned = on16(x.p) && on16(x.g) && on16(x.m) && on16(x.v) && on16(x.copy);
-        d.index = (int)((unsigned int)i | (aligned ? 0x80000000u : 0u));
-        tb.chunks += (unsigned int)((x.n + CHUNK - 1) / CHUNK);
+      if (whole) {
+        i = count;
+      } else {
+        start();
+        for (; i < count && tb.count < ADAM_CAP; ++i)
+          if (t[i].n != 0 && t[i].g && type_class(t[i]) == cls) put(i);
       }
       if (tb.count == 0) break;
       const bool sr = o->stochastic != 0;
@@ -573,27 +583,36 @@ size_t defl_grad_norm_work_bytes(int count) {
 int defl_grad_norm(defl_ctx* c, const defl_norm_tensor* t, int count, float max_norm, float* out, int64_t* step, void* work) {
   if (!c || count < 0 || (count > 0 && !t) || !out || !work || !on(work, 8) || !on(out, 4) || !on(step, 8) || isnan(max_norm)) return DEFL_ERR_ARG;
   unsigned long long total = 0;
+  NormTable<NORM_CAP> tb;
+  auto start = [&] { tb.count = 0; tb.chunks = 0; };
+  auto put = [&](int i) {
+    NormTensor& d = tb.t[tb.count++];
+    d.x = t[i].x; d.n = t[i].n; d.first = tb.chunks;
+    d.dtype = (int)((unsigned int)t[i].dtype | (on16(t[i].x) ? 0x80000000u : 0u));
+    tb.chunks += (unsigned int)((t[i].n + NORM_CHUNK - 1) / NORM_CHUNK);
+  };
+  bool whole = true;                              // as in defl_adamw_step
+  start();
   for (int i = 0; i < count; ++i) {
     if (t[i].n < 0 || t[i].n > MAX_ELEMENTS) return DEFL_ERR_ARG;
     if (t[i].n == 0) continue;
     if (!t[i].x || (t[i].dtype != DEFL_F32 && t[i].dtype != DEFL_BF16) || !on(t[i].x, (unsigned)dtype_size(t[i].dtype))) return DEFL_ERR_ARG;
+    whole = whole && tb.count < NORM_CAP;
+    if (whole) put(i);
     total += (unsigned long long)((t[i].n + NORM_CHUNK - 1) / NORM_CHUNK);
   }
   if (total > 0x7fffffffull) return DEFL_ERR_RANK;
   DeviceScope scope(c->device);
   c->err[0] = 0;
-  NormTable<NORM_CAP> tb;
   double* const partial = reinterpret_cast<double*>(work);
   int slots = 0;
   for (int i = 0; i < count;) {
-    tb.count = 0;
-    tb.chunks = 0;
-    for (; i < count && tb.count < NORM_CAP; ++i) {
-      if (t[i].n == 0) continue;
-      NormTensor& d = tb.t[tb.count++];
-      d.x = t[i].x; d.n = t[i].n; d.first = tb.chunks;
-      d.dtype = (int)((unsigned int)t[i].dtype | (on16(t[i].x) ? 0x80000000u : 0u));
-      tb.chunks += (unsigned int)((t[i].n + NORM_CHUNK - 1) / NORM_CHUNK);
+    if (whole) {
+      i = count;
+    } else {
+      start();
+      for (; i < count && tb.count < NORM_CAP; ++i)
+        if (t[i].n != 0) put(i);
     }
     if (tb.count == 0) break;
     const int grid = tb.chunks < (unsigned int)NORM_BLOCKS ? (int)tb.chunks : NORM_BLOCKS;
